@@ -343,6 +343,149 @@ evisel_status evisel_frame_evidence(const evisel_mask* mask,
                                     const float* frame_pairs, float* e_ff,
                                     void* stream);
 
+/* ---------------------------------------------------------------------------
+ * One layer's key/value cache: what a program answers from after the probe.
+ * evisel_cache_append brings the prefill's keys and values (or those of
+ * accepted drafted tokens) into it, evisel_tree_attention attends over it,
+ * evisel_cache_evict cuts it to a budget by accumulated attention weight.
+ *
+ * The caller owns every buffer and fills this view of them (host memory,
+ * read during the call only). Slots 0 .. length[s] - 1 of sequence s hold
+ * its tokens, slot j at row j % page of page page_table[s][j / page]; the
+ * capacity is max_pages * page. The order of the slots means nothing:
+ * attention does not depend on it, and eviction, which each kv head decides
+ * for itself, moves tokens between slots. pos says which token a slot holds.
+ *   k, v        device, n_pages pages of `page` rows of hkv heads of d
+ *               elements; element (p, r, h, e) at p * page_stride +
+ *               r * token_stride + h * head_stride + e (strides in elements,
+ *               16-byte multiples). Pages of two sequences may be the same
+ *               (a shared prefix) as long as no call writes them.
+ *   page_table  device int32 [n_seq][max_pages]. An entry outside
+ *               [0, n_pages) is no page: its slots hold nothing, take no
+ *               part in attention, and what is written there is dropped.
+ *   length      device int32 [n_seq], tokens held
+ *   seen        device int32 [n_seq], tokens appended so far: the position
+ *               of the next one (append and evict)
+ *   weight      device fp32 [n_seq][hkv][capacity], accumulated attention
+ *               weight (evict; append and attention when given)
+ *   pos         device int32 [n_seq][hkv][capacity] (evict; append when
+ *               given)
+ * Every layer has its own view with its own length, seen, weight and pos.
+ * Requires n_seq >= 1, hkv >= 1, d = 64 or 128, page a power of two from 16
+ * to 2^20, a capacity of at most 2^30 slots, strides of at least d and at
+ * most 2^24 elements (page_stride: any) that keep the rows apart. */
+typedef struct {
+  void* k;
+  void* v;
+  const int32_t* page_table;
+  int32_t* length;
+  int32_t* seen;   /* may be NULL for evisel_tree_attention */
+  float* weight;   /* may be NULL where no weights are kept */
+  int32_t* pos;    /* may be NULL where nothing is evicted  */
+  int64_t n_pages;
+  int64_t page_stride, token_stride, head_stride;
+  int32_t n_seq, hkv, d, page, max_pages;
+  evisel_dtype dtype;
+} evisel_cache;
+
+/* Appends tokens to every sequence: the i-th goes to slot length + i with
+ * position seen + i, then length and seen grow by their number.
+ *   k_new, v_new  device [n_tok, hkv, d], the cache's dtype; sequence s has
+ *             the rows tok_ptr[s] .. tok_ptr[s+1] - 1
+ *   tok_ptr   device int32 [n_seq + 1], increasing
+ *   accept    device int32 [n_tok] or NULL: the i-th appended token of
+ *             sequence s is its row accept[tok_ptr[s] + i] (counted from the
+ *             sequence's first; clamped to its rows) instead of row i
+ *   n_accept  device int32 [n_seq] or NULL: tokens appended, clamped to the
+ *             sequence's rows (NULL: all of them)
+ *   max_new   host: no sequence appends more (the rest is left out)
+ *   w_new     device fp32 [n_tok, hkv] or NULL: the tokens' first weights
+ *             (evisel_tree_attention's w_new, or evidence; NULL: 0)
+ * Tokens past the capacity are left out and not counted.
+ * Errors: INVALID_ARG, UNSUPPORTED (d, dtype, page), HIP. */
+evisel_status evisel_cache_append(const evisel_cache* cache,
+                                  const void* k_new, const void* v_new,
+                                  int32_t n_tok, const int32_t* tok_ptr,
+                                  const int32_t* accept,
+                                  const int32_t* n_accept, int32_t max_new,
+                                  const float* w_new, void* stream);
+
+/* Attention of drafted tokens over the cache: one layer of a step of
+ * generation. Sequence s has the tokens tree_ptr[s] .. tree_ptr[s+1] - 1
+ * (at most 64; none leaves the sequence alone); each sees every cached
+ * token of its sequence, itself, and its ancestors among the drafted ones.
+ * One token per sequence is ordinary generation.
+ *   q         device [n_tok, hq, d], the cache's dtype
+ *   k_new, v_new  device [n_tok, hkv, d]: the drafted tokens' own keys and
+ *             values, or both NULL: the tokens see the cache alone (which
+ *             already holds what they are to see)
+ *   tree_ptr  device int32 [n_seq + 1], increasing, within [0, n_tok]
+ *   parent    device int32 [n_tok] or NULL: index, counted from the
+ *             sequence's first token, of each token's parent; a value
+ *             outside [0, own index) is a root. NULL: a chain (each token
+ *             sees all before it)
+ *   max_tree  host, 1 .. 64: no sequence has more tokens (the rest is left
+ *             out)
+ *   max_len   host, 0 .. capacity: no sequence has more cached tokens (the
+ *             rest is left out). The launch is made for it; in a captured
+ *             graph it bounds the lengths of later replays
+ *   out       device [n_tok, hq, d]: softmax(q k^T * scale) v over the
+ *             keys that each row sees (fp32 accumulation; bf16 inputs: the
+ *             probabilities are rounded to bf16 for the product with v, the
+ *             output to nearest even)
+ *   lse       device fp32 [hq, n_tok] or NULL: natural-log log-sum-exp
+ *   accumulate  != 0: weight[s][g][j] = decay * weight + the sum over the
+ *             sequence's tokens i and the query heads of kv head g of
+ *             vote[i] * softmax weight on slot j (vote NULL: 1; a token with
+ *             vote 0 takes no part), and w_new[t][g], device fp32
+ *             [n_tok, hkv] or NULL, gets the same sum for drafted token t.
+ *             0: vote, decay and w_new are not used, weight is not touched
+ *   workspace device, 256-byte aligned, evisel_tree_attention_workspace
+ *             bytes; calls that may overlap need one each
+ * A row without any key of a logit above -inf gets zeros and lse = -inf.
+ * What a row does not see does not reach it, whatever its values. Rows
+ * outside the sequences are left as they were. Deterministic: no result
+ * depends on the order of the work.
+ * Errors: INVALID_ARG, UNSUPPORTED (d, dtype, page), WORKSPACE, HIP. */
+evisel_status evisel_tree_attention(
+    const evisel_cache* cache, int32_t hq, const void* q, const void* k_new,
+    const void* v_new, int32_t n_tok, const int32_t* tree_ptr,
+    const int32_t* parent, int32_t max_tree, int32_t max_len,
+    float softmax_scale, void* out, float* lse, int32_t accumulate,
+    const float* vote, float decay, float* w_new, void* workspace,
+    size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace of such a call (0 for arguments that it refuses). */
+size_t evisel_tree_attention_workspace(const evisel_cache* cache, int32_t hq,
+                                       int32_t max_tree, int32_t max_len,
+                                       int32_t accumulate);
+
+/* Cuts every sequence with more than `budget` tokens to `budget`. Each kv
+ * head keeps the tokens of position below n_sink, those of the last n_recent
+ * positions (pos >= seen - n_recent), and of the others those with the
+ * largest accumulated weight (NaN ranks as -inf; equal weights: lower slot
+ * first). Kept tokens in slots >= budget move, in slot order, to the slots
+ * below it that became free, in slot order, with their weight and pos; the
+ * other kept tokens stay where they are. Then length = budget. Slots from
+ * the new length on are left as they were, and their pages are the caller's
+ * to reuse.
+ *   budget    host, >= 1, n_sink + n_recent <= budget
+ *   max_len   host, 0 .. capacity: no sequence has more cached tokens (a
+ *             longer one is taken for one of max_len)
+ *   workspace device, 256-byte aligned, evisel_cache_evict_workspace bytes
+ * A page that two sequences share must not be written: give every sequence
+ * pages of its own before it is evicted from.
+ * Errors: INVALID_ARG (seen, weight or pos missing among others),
+ * UNSUPPORTED (d, dtype, page), WORKSPACE, HIP. */
+evisel_status evisel_cache_evict(const evisel_cache* cache, int32_t budget,
+                                 int32_t n_sink, int32_t n_recent,
+                                 int32_t max_len, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace of such a call (0 for arguments that it refuses). */
+size_t evisel_cache_evict_workspace(const evisel_cache* cache, int32_t budget,
+                                    int32_t max_len);
+
 /* Kernel timing, a tracing aid. evisel_profile_begin creates 5 * capacity
  * HIP events on the current device. The evisel_sparse_prefill calls that
  * follow are counted from 0; calls 0, stride, 2 * stride, ... are timed, up

@@ -12,6 +12,12 @@ Entry points (same names as the C ABI):
     frame_evidence         head/layer aggregation and per-video top-k frames
     sparse_prefill_workspace, mask_info, mask_export, mask_export_work,
     mask_export_paired     plan inspection (host tables)
+    Cache                  one layer's paged key/value cache (caller's tensors)
+    cache_append           prefilled or accepted tokens into the cache
+    tree_attention         drafted tokens (or one) over the cache; accumulates
+                           its attention weight
+    cache_evict            cuts the cache to a budget by that weight
+    tree_attention_workspace, cache_evict_workspace     their workspaces
 """
 from __future__ import annotations
 
@@ -26,7 +32,9 @@ __all__ = ["load", "EviselError", "Mask", "build_block_mask",
            "mask_info", "mask_export", "mask_export_work",
            "mask_export_paired", "mask_permute_work", "profile_begin",
            "sparse_prefill_noalloc", "NOALLOC_WORKSPACE_BYTES",
-           "profile_end", "LIB_PATH"]
+           "profile_end", "LIB_PATH", "Cache", "cache_append",
+           "tree_attention", "tree_attention_workspace", "cache_evict",
+           "cache_evict_workspace"]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)),
                         "libevisel.so")
@@ -56,6 +64,16 @@ class _Stats(ctypes.Structure):
                                        "tokens_per_frame", "hist_words")] + \
         [("tau_p", ctypes.c_float), ("n_frame_pairs", ctypes.c_int64),
          ("n_paired_tiles", ctypes.c_int64)]
+
+
+class _CacheView(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in (
+        "k", "v", "page_table", "length", "seen", "weight", "pos")] + \
+        [(n, ctypes.c_int64) for n in ("n_pages", "page_stride",
+                                       "token_stride", "head_stride")] + \
+        [(n, ctypes.c_int32) for n in ("n_seq", "hkv", "d", "page",
+                                       "max_pages")] + \
+        [("dtype", ctypes.c_int)]
 
 
 _lib = None
@@ -106,6 +124,24 @@ _SIGS = {
         ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p,
         ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
         ctypes.c_void_p, ctypes.c_void_p]),
+    "evisel_cache_append": (ctypes.c_int, [
+        ctypes.POINTER(_CacheView), ctypes.c_void_p, ctypes.c_void_p,
+        ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
+        ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p]),
+    "evisel_tree_attention": (ctypes.c_int, [
+        ctypes.POINTER(_CacheView), ctypes.c_int32, ctypes.c_void_p,
+        ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p,
+        ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32, ctypes.c_float,
+        ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p,
+        ctypes.c_float, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t,
+        ctypes.c_void_p]),
+    "evisel_tree_attention_workspace": (ctypes.c_size_t, [
+        ctypes.POINTER(_CacheView)] + [ctypes.c_int32] * 4),
+    "evisel_cache_evict": (ctypes.c_int, [
+        ctypes.POINTER(_CacheView)] + [ctypes.c_int32] * 4 + [
+        ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "evisel_cache_evict_workspace": (ctypes.c_size_t, [
+        ctypes.POINTER(_CacheView)] + [ctypes.c_int32] * 2),
     "evisel_profile_begin": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int32,
                                             ctypes.c_int32]),
     "evisel_profile_end": (ctypes.c_int, [ctypes.POINTER(ctypes.c_double),
@@ -382,6 +418,168 @@ def frame_evidence(mask: Mask, evidence, n_layers: int, e_qf,
     _check(load().evisel_frame_evidence(
         mask.handle, _ptr(evidence), n_layers, _ptr(e_qf_layer), _ptr(e_qf),
         _ptr(k_per_seq), _ptr(topk), _ptr(frame_pairs), _ptr(e_ff),
+        _stream(stream)))
+
+
+def _want(name, t, dtype, *shape):
+    """A dense tensor of this type on the current device, with at least these
+    axes (None: any size)."""
+    import torch
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
+    if t.dim() != len(shape) or any(
+            s is not None and s != g for s, g in zip(shape, t.shape)):
+        raise ValueError(f"{name} has the shape {tuple(t.shape)}, not {shape}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if t.is_cuda and t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is not on the current device")
+
+
+class Cache:
+    """One layer's key/value cache: a view of the caller's tensors, which it
+    keeps alive. ``k`` and ``v`` are pages [n_pages, page, Hkv, d] (bf16 or
+    fp32; the same strides, d contiguous, otherwise any), ``page_table`` int32
+    [n_seq, max_pages], ``length`` and ``seen`` int32 [n_seq], ``weight`` fp32
+    and ``pos`` int32 [n_seq, Hkv, max_pages * page]. Attention needs neither
+    ``seen`` nor ``pos``, and ``weight`` only to accumulate; appending needs
+    ``seen``; eviction all of them."""
+
+    def __init__(self, k, v, page_table, length, seen=None, weight=None,
+                 pos=None):
+        import torch
+        if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or \
+                k.dtype != v.dtype or k.device != v.device:
+            raise ValueError("k and v must be [n_pages, page, Hkv, d], alike "
+                             "in shape, strides, type and device")
+        if k.stride(3) != 1:
+            raise ValueError("the last axis of k and v must be contiguous")
+        if k.is_cuda and k.device.index != torch.cuda.current_device():
+            raise ValueError("the cache is not on the current device")
+        n_pages, page, hkv, d = k.shape
+        i32 = torch.int32
+        _want("page_table", page_table, i32, None, None)
+        n_seq, max_pages = page_table.shape
+        _want("length", length, i32, n_seq)
+        if seen is not None:
+            _want("seen", seen, i32, n_seq)
+        if weight is not None:
+            _want("weight", weight, torch.float32, n_seq, hkv,
+                  max_pages * page)
+        if pos is not None:
+            _want("pos", pos, i32, n_seq, hkv, max_pages * page)
+        self.k, self.v, self.page_table, self.length = k, v, page_table, length
+        self.seen, self.weight, self.pos = seen, weight, pos
+        self.n_seq, self.hkv, self.d, self.page = n_seq, hkv, d, page
+        self.capacity = max_pages * page
+        p = lambda t: None if t is None else t.data_ptr()
+        # the stride of an axis of one is anything: a valid one instead
+        ts = k.stride(1)
+        hs = k.stride(2) if hkv > 1 else d
+        ps = k.stride(0) if n_pages > 1 else max(page * ts, hkv * hs)
+        self._view = _CacheView(p(k), p(v), p(page_table), p(length), p(seen),
+                                p(weight), p(pos), n_pages, ps, ts, hs, n_seq,
+                                hkv, d, page, max_pages, _dtype_code(k))
+        self._ref = ctypes.byref(self._view)
+
+    def _new_tokens(self, k_new, v_new):
+        n = k_new.shape[0]
+        for name, t in (("k_new", k_new), ("v_new", v_new)):
+            _want(name, t, self.k.dtype, n, self.hkv, self.d)
+        return n
+
+
+def cache_append(cache: Cache, k_new, v_new, tok_ptr, max_new: int,
+                 accept=None, n_accept=None, w_new=None, stream=None):
+    """Appends tokens to the sequences: ``k_new``, ``v_new`` [n_tok, Hkv, d],
+    sequence s the rows tok_ptr[s] .. tok_ptr[s+1]-1 (int32 [n_seq + 1]), of
+    which ``accept`` (int32 [n_tok], local indices) and ``n_accept`` (int32
+    [n_seq]) pick some, in order; at most ``max_new`` a sequence. ``w_new``
+    [n_tok, Hkv] fp32: their first accumulated weights (default 0)."""
+    import torch
+    n = cache._new_tokens(k_new, v_new)
+    _want("tok_ptr", tok_ptr, torch.int32, cache.n_seq + 1)
+    if accept is not None:
+        _want("accept", accept, torch.int32, n)
+    if n_accept is not None:
+        _want("n_accept", n_accept, torch.int32, cache.n_seq)
+    if w_new is not None:
+        _want("w_new", w_new, torch.float32, n, cache.hkv)
+    _check(load().evisel_cache_append(
+        cache._ref, _ptr(k_new), _ptr(v_new), n, _ptr(tok_ptr), _ptr(accept),
+        _ptr(n_accept), int(max_new), _ptr(w_new), _stream(stream)))
+
+
+def tree_attention_workspace(cache: Cache, hq: int, max_tree: int,
+                             max_len: int, accumulate: bool = False) -> int:
+    """Workspace bytes of a tree_attention call with these bounds
+    (``accumulate``: with ``decay``)."""
+    return int(load().evisel_tree_attention_workspace(
+        cache._ref, hq, max_tree, max_len, int(bool(accumulate))))
+
+
+def tree_attention(cache: Cache, q, k_new, v_new, tree_ptr, out, workspace,
+                   max_tree: int, max_len: int, parent=None, lse=None,
+                   vote=None, decay: Optional[float] = None, w_new=None,
+                   softmax_scale: Optional[float] = None, stream=None):
+    """Attention of drafted tokens over the cache and their own tree: ``q``,
+    ``out`` [n_tok, Hq, d], ``k_new``, ``v_new`` [n_tok, Hkv, d] (or both
+    None: the cache alone), sequence s the rows tree_ptr[s] ..
+    tree_ptr[s+1]-1 (int32 [n_seq + 1]), ``parent`` int32 [n_tok] (local
+    index of each token's parent, negative for a root; None: chains), ``lse``
+    [Hq, n_tok] fp32. No sequence has more than ``max_tree`` (<= 64) tokens or
+    ``max_len`` cached ones. With ``decay`` the cache's weight becomes decay *
+    weight + the attention weight of the call's rows, each token's times
+    ``vote`` (fp32 [n_tok], default 1), and ``w_new`` [n_tok, Hkv] fp32 gets
+    the drafted tokens' own. ``workspace``: a uint8 tensor of
+    tree_attention_workspace bytes."""
+    import torch
+    n, hq, d = q.shape
+    _want("q", q, cache.k.dtype, None, None, cache.d)
+    _want("out", out, cache.k.dtype, n, hq, d)
+    if (k_new is None) != (v_new is None):
+        raise ValueError("k_new and v_new come together")
+    if k_new is not None and cache._new_tokens(k_new, v_new) != n:
+        raise ValueError("k_new needs one row per row of q")
+    _want("tree_ptr", tree_ptr, torch.int32, cache.n_seq + 1)
+    if parent is not None:
+        _want("parent", parent, torch.int32, n)
+    f32 = torch.float32
+    if lse is not None:
+        _want("lse", lse, f32, hq, n)
+    if vote is not None:
+        _want("vote", vote, f32, n)
+    if w_new is not None:
+        _want("w_new", w_new, f32, n, cache.hkv)
+    if decay is None and (vote is not None or w_new is not None):
+        raise ValueError("vote and w_new need decay")
+    scale = float(softmax_scale) if softmax_scale is not None else d ** -0.5
+    _check(load().evisel_tree_attention(
+        cache._ref, hq, _ptr(q), _ptr(k_new), _ptr(v_new), n, _ptr(tree_ptr),
+        _ptr(parent), int(max_tree), int(max_len), scale, _ptr(out),
+        _ptr(lse), int(decay is not None), _ptr(vote),
+        0.0 if decay is None else float(decay), _ptr(w_new), _ptr(workspace),
+        0 if workspace is None else workspace.numel() * workspace.element_size(),
+        _stream(stream)))
+
+
+def cache_evict_workspace(cache: Cache, budget: int, max_len: int) -> int:
+    """Workspace bytes of a cache_evict call with these bounds."""
+    return int(load().evisel_cache_evict_workspace(cache._ref, budget,
+                                                   max_len))
+
+
+def cache_evict(cache: Cache, budget: int, workspace, n_sink: int = 0,
+                n_recent: int = 0, max_len: Optional[int] = None,
+                stream=None):
+    """Cuts every sequence to ``budget`` tokens per kv head: its first
+    ``n_sink``, its last ``n_recent``, and the largest accumulated weights.
+    No sequence has more than ``max_len`` tokens (default: the capacity).
+    ``workspace``: a uint8 tensor of cache_evict_workspace bytes."""
+    _check(load().evisel_cache_evict(
+        cache._ref, int(budget), int(n_sink), int(n_recent),
+        cache.capacity if max_len is None else int(max_len), _ptr(workspace),
+        0 if workspace is None else workspace.numel() * workspace.element_size(),
         _stream(stream)))
 
 

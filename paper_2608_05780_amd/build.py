@@ -16,7 +16,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libevisel.so")
 SOURCES = ["api.hip", "attn.hip", "attn_pipe.hip", "evidence.hip", "select.hip",
-           "plan.cpp"]
+           "cache_api.hip", "cache.hip", "cache_attn.hip", "plan.cpp"]
 HIP_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     # no packed-fp32 VALU instructions anywhere in device code

@@ -6,6 +6,7 @@
 #include <string>
 #include <vector>
 
+#include "cache.h"
 #include "evisel.h"
 #include "kernels.h"
 #include "plan.h"
@@ -43,6 +44,32 @@ evisel_status hip_fail(hipError_t e, const char* what) {
 }
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
+
+}  // namespace
+
+namespace evisel {
+
+evisel_status set_error(evisel_status s, const char* msg) {
+  try {
+    return fail(s, msg);
+  } catch (const std::bad_alloc&) {
+    g_err.clear();   // the status says enough
+    return s;
+  }
+}
+
+evisel_status set_hip_error(hipError_t e, const char* what) {
+  try {
+    return hip_fail(e, what);
+  } catch (const std::bad_alloc&) {
+    g_err.clear();
+    return EVISEL_ERR_HIP;
+  }
+}
+
+}  // namespace evisel
+
+namespace {
 
 struct WsLayout {
   size_t pO, pM, pL, pNV, seg, kbar, rbits, ubits, cpart, total;

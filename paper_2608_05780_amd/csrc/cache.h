@@ -1,0 +1,107 @@
+// The key/value cache: device view and kernel launchers (cache.hip,
+// cache_attn.hip), called from cache_api.hip.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <cstddef>
+#include <cstdint>
+#include <string>
+
+#include "evisel.h"
+
+namespace evisel {
+
+// Records the message of a failing call (api.hip) and returns its status.
+evisel_status set_error(evisel_status s, const char* msg);
+evisel_status set_hip_error(hipError_t e, const char* what);
+
+// Device view of a cache, strides in bytes.
+struct CacheView {
+  char* k;
+  char* v;
+  const int32_t* table;
+  int32_t* length;
+  int32_t* seen;
+  float* weight;
+  int32_t* pos;
+  int64_t n_pages;
+  int64_t page_bytes, head_bytes;
+  int32_t token_bytes;
+  int32_t n_seq, hkv, d;
+  int32_t page_shift, max_pages;
+  int64_t cap;          // max_pages << page_shift
+  int32_t fp32;
+};
+
+// Slots of a sequence that a call looks at.
+__device__ __forceinline__ int held(const CacheView& c, int seq,
+                                    int most) {
+  return min(max(c.length[seq], 0), most);
+}
+
+// Address of row `slot` (kv head 0) from the pool's base, or -1: no page.
+__device__ __forceinline__ int64_t slot_offset(const CacheView& c, int seq,
+                                               int slot) {
+  const int id = c.table[(int64_t)seq * c.max_pages + (slot >> c.page_shift)];
+  if (id < 0 || id >= c.n_pages) return -1;
+  return id * c.page_bytes +
+         (int64_t)(slot & ((1 << c.page_shift) - 1)) * c.token_bytes;
+}
+
+struct AppendCall {
+  const char* k_new;
+  const char* v_new;
+  const int32_t* tok_ptr;
+  const int32_t* accept;     // may be null
+  const int32_t* n_accept;   // may be null
+  const float* w_new;        // may be null
+  int32_t n_tok, max_new;
+};
+hipError_t launch_cache_append(const CacheView& c, const AppendCall& a,
+                               hipStream_t s);
+
+struct EvictCall {
+  int32_t budget, n_sink, n_recent, max_len;
+  int32_t max_moves;   // min(budget, max_len - budget)
+  int32_t* count;      // [n_seq][hkv] moves
+  int32_t* from;       // [n_seq][hkv][max_moves] slots
+  int32_t* to;
+};
+hipError_t launch_cache_evict(const CacheView& c, const EvictCall& e,
+                              hipStream_t s);
+
+// How a tree attention call is split (host, from its bounds alone).
+struct TreePlan {
+  int32_t rows;        // most query rows of a kv head: group * max_tree
+  int32_t row_tiles;   // 16-row tiles that a wave takes (1, 2 or 4)
+  int32_t row_blocks;  // blocks of 16 * row_tiles rows
+  int32_t splits;      // of the keys
+  int32_t stored;      // accumulate: the scores pass through the workspace
+  int64_t len_pad;     // max_len rounded up, of the stored scores
+  // workspace offsets and total, bytes
+  size_t pO, pM, pL, score, total;
+};
+
+struct TreeCall {
+  const char* q;
+  const char* k_new;         // may be null, with v_new
+  const char* v_new;
+  const int32_t* tree_ptr;
+  const int32_t* parent;     // null: chains
+  char* out;
+  float* lse;                // may be null
+  const float* vote;         // may be null
+  float* w_new;              // may be null
+  float scale_log2, decay;
+  int32_t hq, n_tok, max_tree, max_len, accumulate;
+  float* pO;                 // [seq][kv head][split][row][d]
+  float* pM;                 // [seq][kv head][split][row], log2 units
+  float* pL;
+  float* score;              // [seq][kv head][row][len_pad + 64], log2 units
+};
+TreePlan plan_tree(const CacheView& c, int32_t hq, int32_t max_tree,
+                   int32_t max_len, int32_t accumulate);
+hipError_t launch_tree_attention(const CacheView& c, const TreePlan& p,
+                                 const TreeCall& t, hipStream_t s);
+
+}  // namespace evisel

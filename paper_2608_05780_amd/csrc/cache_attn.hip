@@ -1,0 +1,977 @@
+// Attention of drafted tokens over a paged cache, its join over the splits,
+// and the accumulated attention weight.
+#include <algorithm>
+
+#include "cache.h"
+
+namespace evisel {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kWaves = 4;
+constexpr int kThreads = 64 * kWaves;
+constexpr int kMaxTree = 64;
+constexpr float kLn2 = 0.69314718055994530942f;
+// A row's reference moves when a logit passes it by this (log2 units): the
+// probabilities stay below 2^8, and fp32 sums and bf16 probabilities keep
+// their relative precision at any such scale.
+constexpr float kSlack = 8.0f;
+// Key tiles a split has at least.
+constexpr int kMinTiles = 4;
+
+__device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
+__device__ __forceinline__ float exp2_(float x) {
+  return __builtin_amdgcn_exp2f(x);
+}
+__device__ __forceinline__ float log2_(float x) {
+  return __builtin_amdgcn_logf(x);
+}
+// Over the four lanes that hold one query row (lane % 16).
+__device__ __forceinline__ float row_max(float x) {
+  x = fmaxf(x, __shfl_xor(x, 16));
+  return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ float row_sum(float x) {
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
+}
+
+// The two operand paths. Both products keep the query row in the lane:
+// S^T = K Q^T leaves lane (c = lane % 16, g = lane / 16) with the logits of
+// row c for the keys 4g .. 4g + 3 of every 16, and O^T += V^T P^T takes P
+// from exactly those registers. K's operand is 16 bytes of key c a step and
+// comes from memory as it is. V's operand wants several keys at one column:
+// a lane reads the columns of chunk c of the keys that it holds logits of,
+// and turns the small square around in its registers. So nothing passes
+// through LDS or waits at a barrier between the pages and the matrix cores.
+template <int D>
+struct TreeBf16 {
+  static constexpr int ES = 2, KT = 32, NH = 2;
+  static constexpr int KS = D * ES / 64;   // 64-byte steps of a row
+  static constexpr int VC = D / 16;        // columns of a lane's V chunk
+  static constexpr int NT = D / 16;        // 16-column tiles of O^T
+  typedef uint32_t chunk __attribute__((ext_vector_type(VC / 2)));
+  struct Row {
+    bf16x8 x[KS];
+  };
+  struct Val {
+    chunk x[NH][4];
+  };
+  // V's lane offset within a row, and O's column of (g, i, t)
+  static constexpr int kLaneV = VC * ES;
+  static __device__ int col(int g, int i, int t) {
+    return VC * (4 * g + i) + t;
+  }
+  static __device__ void load_row(Row& r, const char* p) {
+#pragma unroll
+    for (int j = 0; j < KS; ++j) r.x[j] = *(const bf16x8*)(p + 64 * j);
+  }
+  static __device__ void load_val(chunk& v, const char* p) {
+    v = *(const chunk*)p;
+  }
+  static __device__ void zero_val(chunk& v) { v = chunk{}; }
+  static __device__ void zero_row(Row& r) {
+#pragma unroll
+    for (int j = 0; j < KS; ++j) r.x[j] = bf16x8{};
+  }
+  static __device__ f32x4 qk(const Row& k, const Row& q) {
+    f32x4 s = {};
+#pragma unroll
+    for (int j = 0; j < KS; ++j)
+      s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k.x[j], q.x[j], s, 0, 0, 0);
+    return s;
+  }
+  // The A operands of V^T, for every column of the chunk its eight keys: 4g ..
+  // 4g + 3 of the first 16, then of the second.
+  struct ValT {
+    bf16x8 x[NT];
+  };
+  static __device__ void turn(ValT& o, const Val& v) {
+#pragma unroll
+    for (int w = 0; w < VC / 2; ++w) {
+      u32x4 lo, hi;
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        const uint32_t a = v.x[p / 2][2 * (p % 2)][w];
+        const uint32_t b = v.x[p / 2][2 * (p % 2) + 1][w];
+        lo[p] = __builtin_amdgcn_perm(b, a, 0x05040100u);
+        hi[p] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+      }
+      o.x[2 * w] = __builtin_bit_cast(bf16x8, lo);
+      o.x[2 * w + 1] = __builtin_bit_cast(bf16x8, hi);
+    }
+  }
+  static __device__ void pv(f32x4 (&o)[NT], const ValT& v,
+                            const f32x4 (&p)[NH]) {
+    const f32x8 pf = __builtin_shufflevector(p[0], p[1], 0, 1, 2, 3, 4, 5, 6, 7);
+    // rounded to bf16 for the matrix cores: half a step, 2^-9 of a
+    // probability, and independent from key to key
+    const bf16x8 pb = __builtin_convertvector(pf, bf16x8);
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+      o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.x[t], pb, o[t], 0, 0, 0);
+  }
+  static __device__ bool finite(const chunk& v) {
+    bool ok = true;
+#pragma unroll
+    for (int w = 0; w < VC / 2; ++w)
+      ok = ok && (v[w] & 0x7F80u) != 0x7F80u &&
+           (v[w] & 0x7F800000u) != 0x7F800000u;
+    return ok;
+  }
+  static __device__ void drop_infinite(chunk& v) {
+#pragma unroll
+    for (int w = 0; w < VC / 2; ++w) {
+      if ((v[w] & 0x7F80u) == 0x7F80u) v[w] &= 0xFFFF0000u;
+      if ((v[w] & 0x7F800000u) == 0x7F800000u) v[w] &= 0xFFFFu;
+    }
+  }
+  static __device__ float element(const char* row, int e) {
+    return __uint_as_float((uint32_t)((const uint16_t*)row)[e] << 16);
+  }
+  static __device__ void store(char* dst, const float (&x)[D / 16]) {
+    typedef __bf16 out_t __attribute__((ext_vector_type(D / 16)));
+    typedef float in_t __attribute__((ext_vector_type(D / 16)));
+    in_t v;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) v[i] = x[i];
+    *(out_t*)dst = __builtin_convertvector(v, out_t);
+  }
+};
+
+template <int D>
+struct TreeF32 {
+  static constexpr int ES = 4, KT = 16, NH = 1;
+  static constexpr int KS = D * ES / 64;
+  static constexpr int NT = D / 16;
+  static constexpr int NC = D / 64;        // 16-byte chunks of V per lane
+  struct chunk {
+    f32x4 x[NC];
+  };
+  struct Row {
+    f32x4 x[KS];
+  };
+  struct Val {
+    chunk x[NH][4];
+  };
+  static constexpr int kLaneV = 16;
+  static __device__ int col(int g, int i, int t) {
+    return 64 * (t / 4) + 4 * (4 * g + i) + t % 4;
+  }
+  static __device__ void load_row(Row& r, const char* p) {
+#pragma unroll
+    for (int j = 0; j < KS; ++j) r.x[j] = *(const f32x4*)(p + 64 * j);
+  }
+  static __device__ void load_val(chunk& v, const char* p) {
+#pragma unroll
+    for (int j = 0; j < NC; ++j) v.x[j] = *(const f32x4*)(p + 256 * j);
+  }
+  static __device__ void zero_val(chunk& v) { v = chunk{}; }
+  static __device__ void zero_row(Row& r) {
+#pragma unroll
+    for (int j = 0; j < KS; ++j) r.x[j] = f32x4{};
+  }
+  static __device__ f32x4 qk(const Row& k, const Row& q) {
+    f32x4 s = {};
+#pragma unroll
+    for (int j = 0; j < KS; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        s = __builtin_amdgcn_mfma_f32_16x16x4f32(k.x[j][e], q.x[j][e], s, 0, 0,
+                                                 0);
+    return s;
+  }
+  typedef Val ValT;   // one key a step: as it came
+  static __device__ void turn(ValT& o, const Val& v) { o = v; }
+  static __device__ void pv(f32x4 (&o)[NT], const ValT& v,
+                            const f32x4 (&p)[NH]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+        o[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(v.x[0][i].x[t / 4][t % 4],
+                                                    p[0][i], o[t], 0, 0, 0);
+  }
+  static __device__ bool finite(const chunk& v) {
+    bool ok = true;
+#pragma unroll
+    for (int j = 0; j < NC; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) ok = ok && __builtin_isfinite(v.x[j][e]);
+    return ok;
+  }
+  static __device__ void drop_infinite(chunk& v) {
+#pragma unroll
+    for (int j = 0; j < NC; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (!__builtin_isfinite(v.x[j][e])) v.x[j][e] = 0.f;
+  }
+  static __device__ float element(const char* row, int e) {
+    return ((const float*)row)[e];
+  }
+  static __device__ void store(char* dst, const float (&x)[D / 16]) {
+#pragma unroll
+    for (int i = 0; i < D / 16; i += 4) {
+      const f32x4 v = {x[i], x[i + 1], x[i + 2], x[i + 3]};
+      *(f32x4*)(dst + 4 * i) = v;
+    }
+  }
+};
+
+struct Yes {
+  static constexpr bool value = true;
+};
+struct No {
+  static constexpr bool value = false;
+};
+
+// The page table is not written while a kernel reads it: scalar loads.
+typedef const __attribute__((address_space(4))) int32_t* ScalarTable;
+
+// A sequence's part of a call.
+struct Tree {
+  int first, n;   // its rows of q and their number
+  int len;        // cached tokens
+};
+__device__ __forceinline__ Tree tree_of(const CacheView& c, const TreeCall& t,
+                                        int seq) {
+  Tree r;
+  r.first = min(max(t.tree_ptr[seq], 0), t.n_tok);
+  r.n = min(max(t.tree_ptr[seq + 1], r.first), t.n_tok) - r.first;
+  r.n = min(r.n, t.max_tree);
+  r.len = held(c, seq, t.max_len);
+  return r;
+}
+
+// Tiles of the cache and of the drafted tokens, and how many of them each of
+// `splits` parts takes.
+struct Parts {
+  int cached, total, per, used;
+};
+__device__ __forceinline__ Parts parts_of(const Tree& r, bool drafts, int kt,
+                                          int splits) {
+  Parts p;
+  p.cached = (r.len + kt - 1) / kt;
+  p.total = p.cached + (drafts ? (r.n + kt - 1) / kt : 0);
+  p.per = max((p.total + splits - 1) / splits, kMinTiles);
+  p.used = max((p.total + p.per - 1) / p.per, 1);
+  return p;
+}
+
+// Which drafted tokens token `lane` sees: itself and its ancestors. The lanes'
+// parents are followed by doubling, six times for 64 tokens.
+__device__ __forceinline__ uint64_t ancestors(const TreeCall& t, const Tree& r,
+                                              int lane) {
+  if (!t.parent) return ~0ull >> (63 - lane);
+  int up = lane < r.n ? t.parent[r.first + lane] : -1;
+  if (up < 0 || up >= lane) up = lane;   // a root sees itself
+  uint64_t m = 1ull << lane;
+#pragma unroll
+  for (int i = 0; i < 6; ++i) {
+    m |= __shfl(m, up);
+    up = __shfl(up, up);
+  }
+  return m;
+}
+
+// A tile's rows in memory: address of the first key of every 16 (K's pool and
+// V's alike) and how many of the 16 are there.
+template <int NH>
+struct Where {
+  int64_t off[NH];
+  int n[NH];
+};
+template <int NH>
+__device__ __forceinline__ void find(Where<NH>& w, const CacheView& c, int seq,
+                                     int64_t head, int len, int slot0) {
+#pragma unroll
+  for (int h = 0; h < NH; ++h) {
+    const int s = slot0 + 16 * h;
+    w.off[h] = head;
+    w.n[h] = 0;
+    if (s < len) {
+      const int id = ((ScalarTable)c.table)[(int64_t)seq * c.max_pages +
+                                            (s >> c.page_shift)];
+      if (id >= 0 && id < c.n_pages) {
+        w.off[h] = id * c.page_bytes + head +
+                   (int64_t)(s & ((1 << c.page_shift) - 1)) * c.token_bytes;
+        w.n[h] = min(16, len - s);
+      }
+    }
+  }
+}
+
+template <class P>
+__device__ __forceinline__ void fetch_k(typename P::Row (&k)[P::NH],
+                                        const CacheView& c,
+                                        const Where<P::NH>& at,
+                                        uint32_t koff) {
+#pragma unroll
+  for (int h = 0; h < P::NH; ++h) P::load_row(k[h], c.k + at.off[h] + koff);
+}
+template <class P>
+__device__ __forceinline__ void fetch_v(typename P::Val& v, const CacheView& c,
+                                        const Where<P::NH>& at,
+                                        uint32_t voff) {
+#pragma unroll
+  for (int h = 0; h < P::NH; ++h)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      P::load_val(v.x[h][i], c.v + at.off[h] + (voff + i * c.token_bytes));
+}
+
+// One wavefront's running softmax over RT tiles of 16 query rows.
+template <class P, int D, int RT>
+struct Rows {
+  typename P::Row q[RT];
+  f32x4 o[RT][P::NT];
+  float m[RT], l[RT];   // reference and sum, log2 units
+
+  // Logits of a tile of keys; score: where they go, or null. vis[rt]: bit
+  // 4h + i set if the row sees key 16h + 4g + i (all: every row sees every
+  // key).
+  __device__ __forceinline__ void logits(f32x4 (&x)[RT][P::NH],
+                                         const typename P::Row (&k)[P::NH],
+                                         float scale) {
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+      for (int h = 0; h < P::NH; ++h) x[rt][h] = P::qk(k[h], q[rt]) * scale;
+  }
+  __device__ __forceinline__ static void hide(f32x4 (&x)[RT][P::NH],
+                                              const uint32_t (&vis)[RT]) {
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+      for (int h = 0; h < P::NH; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (!(vis[rt] >> (4 * h + i) & 1)) x[rt][h][i] = neg_inf();
+  }
+  // Logits to probabilities (against the rows' references) and their sums.
+  __device__ __forceinline__ void softmax(f32x4 (&x)[RT][P::NH]) {
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      float top = neg_inf();
+#pragma unroll
+      for (int h = 0; h < P::NH; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, x[rt][h][i]);
+      if (__any(top > m[rt] + kSlack)) {
+        const float next = fmaxf(m[rt], row_max(top));
+        const float a = m[rt] == neg_inf() ? 0.f : exp2_(m[rt] - next);
+        m[rt] = next;
+        l[rt] *= a;
+#pragma unroll
+        for (int t = 0; t < P::NT; ++t) o[rt][t] *= a;
+      }
+      const float ref = m[rt] == neg_inf() ? 0.f : m[rt];
+#pragma unroll
+      for (int h = 0; h < P::NH; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x[rt][h][i] = exp2_(x[rt][h][i] - ref);
+          l[rt] += x[rt][h][i];
+        }
+    }
+  }
+  __device__ __forceinline__ void add(const typename P::ValT& v,
+                                      const f32x4 (&x)[RT][P::NH]) {
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) P::pv(o[rt], v, x[rt]);
+  }
+};
+
+// One work-group: a sequence, a kv head, a run of its key tiles (a split) and
+// 16 RT of its query rows. The wavefronts take the run's tiles in turn, each
+// with the next tile's rows on their way while it works on one, and are
+// joined in LDS at the end. What a run's rows come to is the output, if the
+// sequence has one run, or a partial sum in the workspace.
+template <class P, int D, int RT, bool SCORE>
+__global__ __launch_bounds__(kThreads, RT == 4 ? 1 : 2) void tree_kernel(
+    const CacheView c, const TreePlan pl, const TreeCall t) {
+  constexpr int KT = P::KT, NH = P::NH;
+  constexpr int kPad = D + 4;
+  // a wavefront's share of one row tile's O, or its probabilities of a tile
+  constexpr int kOwn = RT * KT > kPad ? 16 * RT * KT : 16 * kPad;
+  __shared__ __attribute__((aligned(16))) float so[kWaves][kOwn];
+  __shared__ float sm[kWaves][16 * RT], sl[kWaves][16 * RT];
+  // consecutive work-groups go to the 8 XCDs in turn; the row blocks of one
+  // run stay on one of them, whose L2 then serves the run's keys again
+  const int xcd = blockIdx.x % 8, y = blockIdx.x / 8;
+  const int rb = y % pl.row_blocks;
+  int unit = y / pl.row_blocks * 8 + xcd;
+  if (unit >= c.n_seq * c.hkv * pl.splits) return;
+  const int split = unit % pl.splits;
+  unit /= pl.splits;
+  const int kvh = unit % c.hkv, seq = unit / c.hkv;
+  const Tree tr = tree_of(c, t, seq);
+  const int group = t.hq / c.hkv, n_rows = tr.n * group;
+  const int row0 = rb * 16 * RT;
+  if (row0 >= n_rows) return;
+  const Parts pt = parts_of(tr, t.k_new != nullptr, KT, pl.splits);
+  if (split >= pt.used) return;
+  const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int t0 = split * pt.per, t1 = min(t0 + pt.per, pt.total);
+  const int64_t head = kvh * c.head_bytes;
+  const uint32_t koff = (uint32_t)c16 * c.token_bytes + 16 * g;
+  const uint32_t voff = (uint32_t)(4 * g) * c.token_bytes + c16 * P::kLaneV;
+
+  Rows<P, D, RT> rows;
+  float* score[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int r = row0 + 16 * rt + c16;
+    rows.m[rt] = neg_inf();
+    rows.l[rt] = 0.f;
+#pragma unroll
+    for (int i = 0; i < P::NT; ++i) rows.o[rt][i] = f32x4{};
+    if (r < n_rows) {
+      const int tok = r / group, qh = r % group;
+      P::load_row(rows.q[rt],
+                  t.q + ((int64_t)(tr.first + tok) * t.hq + kvh * group + qh) *
+                            (D * P::ES) + 16 * g);
+    } else {
+      P::zero_row(rows.q[rt]);
+    }
+    score[rt] = SCORE && r < n_rows
+                    ? t.score + ((int64_t)unit * pl.rows + r) *
+                                    (pl.len_pad + kMaxTree) + 4 * g
+                    : nullptr;
+  }
+
+  const int c_end = min(t1, pt.cached);
+  int tile = t0 + wave;
+  if (tile < c_end) {
+    const int end = min(tr.len, c_end * KT);
+    typename P::Row k[NH];
+    typename P::Val v;
+    Where<NH> at, next;
+    find<NH>(at, c, seq, head, end, tile * KT);
+    fetch_k<P>(k, c, at, koff);
+    fetch_v<P>(v, c, at, voff);
+    // K's and V's registers are refilled as soon as a product has read them
+    auto take = [&](auto more) {
+      constexpr bool kMore = decltype(more)::value;
+      if (kMore) find<NH>(next, c, seq, head, end, (tile + kWaves) * KT);
+      f32x4 x[RT][NH];
+      rows.logits(x, k, t.scale_log2);
+      if (kMore) fetch_k<P>(k, c, next, koff);
+      bool full = true;
+#pragma unroll
+      for (int h = 0; h < NH; ++h) full = full && at.n[h] == 16;
+      if (!full) {
+        // keys past the end, or without a page: no row sees them, and their
+        // values, whatever they are, must not meet a probability of zero
+        uint32_t vis[RT] = {};
+#pragma unroll
+        for (int h = 0; h < NH; ++h)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if (4 * g + i < at.n[h])
+              vis[0] |= 1u << (4 * h + i);
+            else
+              P::zero_val(v.x[h][i]);
+          }
+#pragma unroll
+        for (int rt = 1; rt < RT; ++rt) vis[rt] = vis[0];
+        rows.hide(x, vis);
+      }
+      if (SCORE && score[0])
+#pragma unroll
+        for (int h = 0; h < NH; ++h)
+          *(f32x4*)(score[0] + (int64_t)tile * KT + 16 * h) = x[0][h];
+      rows.softmax(x);
+      typename P::ValT vt;
+      P::turn(vt, v);
+      if (kMore) fetch_v<P>(v, c, next, voff);
+      rows.add(vt, x);
+      at = next;
+    };
+    for (; tile + kWaves < c_end; tile += kWaves) take(Yes{});
+    take(No{});
+  }
+  for (tile = t0 + wave; tile < t1; tile += kWaves) {
+    if (tile < pt.cached) continue;
+    // drafted tokens: every row has keys of its own
+    const int j0 = (tile - pt.cached) * KT;
+    const uint64_t anc = ancestors(t, tr, lane);
+    const int64_t step = (int64_t)c.hkv * (D * P::ES);
+    const int64_t base = (int64_t)tr.first * step + kvh * (D * P::ES);
+    struct {
+      typename P::Row k[NH];
+      typename P::Val v;
+    } x;
+    bool fine = true;
+#pragma unroll
+    for (int h = 0; h < NH; ++h) {
+      const int j = min(j0 + 16 * h + c16, tr.n - 1);
+      P::load_row(x.k[h], t.k_new + base + j * step + 16 * g);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int jv = j0 + 16 * h + 4 * g + i;
+        if (jv < tr.n) {
+          P::load_val(x.v.x[h][i], t.v_new + base + jv * step + c16 * P::kLaneV);
+          fine = fine && P::finite(x.v.x[h][i]);
+        } else {
+          P::zero_val(x.v.x[h][i]);
+        }
+      }
+    }
+    uint32_t vis[RT];
+    uint32_t sees[RT];   // by key of the tile
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const int r = row0 + 16 * rt + c16;
+      const uint64_t all = __shfl(anc, min(r, n_rows - 1) / group);
+      sees[rt] = r < n_rows ? (uint32_t)(all >> j0) : 0u;
+      vis[rt] = 0;
+#pragma unroll
+      for (int h = 0; h < NH; ++h)
+        vis[rt] |= (sees[rt] >> (16 * h + 4 * g) & 15u) << (4 * h);
+    }
+    f32x4 p[RT][NH];
+    rows.logits(p, x.k, t.scale_log2);
+    rows.hide(p, vis);
+    if (SCORE && score[0])
+#pragma unroll
+      for (int h = 0; h < NH; ++h)
+        *(f32x4*)(score[0] + pl.len_pad + j0 + 16 * h) = p[0][h];
+    rows.softmax(p);
+    // A value that is not finite reaches the rows that see its token and no
+    // other: it is left out of the product, whose zeros it would spoil, and
+    // added by itself.
+    const bool plain = __all(fine);
+    if (!plain) {
+#pragma unroll
+      for (int h = 0; h < NH; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) P::drop_infinite(x.v.x[h][i]);
+    }
+    typename P::ValT vt;
+    P::turn(vt, x.v);
+    rows.add(vt, p);
+    if (plain) continue;
+    float* probs = so[wave];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+      for (int h = 0; h < NH; ++h)
+        *(f32x4*)(probs + (16 * rt + c16) * KT + 16 * h + 4 * g) = p[rt][h];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    for (int j = 0; j < KT && j0 + j < tr.n; ++j) {
+      const char* v = t.v_new + base + (j0 + j) * step;
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        if (!(sees[rt] >> j & 1)) continue;
+        const float pj = probs[(16 * rt + c16) * KT + j];
+#pragma unroll
+        for (int u = 0; u < P::NT; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float e = P::element(v, P::col(g, i, u));
+            if (!__builtin_isfinite(e)) rows.o[rt][u][i] += pj * e;
+          }
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+
+  // the four wavefronts' rows
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    rows.l[rt] = row_sum(rows.l[rt]);
+    if (g == 0) {
+      sm[wave][16 * rt + c16] = rows.m[rt];
+      sl[wave][16 * rt + c16] = rows.l[rt];
+    }
+  }
+  __syncthreads();
+  const int er = threadIdx.x / 16, ec = threadIdx.x % 16;   // row, columns
+  const int64_t part = ((int64_t)unit * pl.splits + split) *
+                       (pl.row_blocks * 16 * RT);
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    float top = neg_inf();
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sm[w][16 * rt + c16]);
+    const float f =
+        rows.m[rt] == neg_inf() ? 0.f : exp2_(rows.m[rt] - top);
+#pragma unroll
+    for (int u = 0; u < P::NT; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        so[wave][c16 * kPad + P::col(g, i, u)] = rows.o[rt][u][i] * f;
+    __syncthreads();
+    const int r = row0 + 16 * rt + er;
+    if (r < n_rows) {
+      float big = neg_inf(), sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w)
+        big = fmaxf(big, sm[w][16 * rt + er]);
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float mw = sm[w][16 * rt + er];
+        sum += (mw == neg_inf() ? 0.f : exp2_(mw - big)) * sl[w][16 * rt + er];
+      }
+      float x[D / 16] = {};
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w)
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i)
+          x[i] += so[w][er * kPad + ec * (D / 16) + i];
+      if (pt.used == 1) {
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) x[i] *= inv;
+        const int tok = r / group, h = kvh * group + r % group;
+        P::store(t.out + ((int64_t)(tr.first + tok) * t.hq + h) * (D * P::ES) +
+                     ec * (D / 16) * P::ES, x);
+        if (t.lse && ec == 0)
+          t.lse[(int64_t)h * t.n_tok + tr.first + tok] =
+              sum == 0.f ? neg_inf() : (big + log2_(sum)) * kLn2;
+      } else {
+        float* dst = t.pO + (part + r) * D + ec * (D / 16);
+#pragma unroll
+        for (int i = 0; i < D / 16; i += 4)
+          *(f32x4*)(dst + i) = f32x4{x[i], x[i + 1], x[i + 2], x[i + 3]};
+      }
+      if (ec == 0 && (pt.used > 1 || t.accumulate)) {
+        t.pM[part + r] = big;
+        t.pL[part + r] = sum;
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// log2 of a row's whole sum, from its splits.
+__device__ __forceinline__ float row_lse2(const TreeCall& t, int64_t base,
+                                          int64_t stride, int used) {
+  float big = neg_inf(), sum = 0.f;
+  for (int s = 0; s < used; ++s) big = fmaxf(big, t.pM[base + s * stride]);
+  for (int s = 0; s < used; ++s) {
+    const float m = t.pM[base + s * stride];
+    sum += (m == neg_inf() ? 0.f : exp2_(m - big)) * t.pL[base + s * stride];
+  }
+  return sum == 0.f ? neg_inf() : big + log2_(sum);
+}
+
+// The splits of a row joined, D / 4 threads a row.
+template <class P, int D>
+__device__ __forceinline__ void join_rows(const CacheView& c,
+                                          const TreePlan& pl,
+                                          const TreeCall& t, int64_t row) {
+  const int padded = pl.row_blocks * 16 * pl.row_tiles;
+  const int unit = (int)(row / pl.rows), r = (int)(row % pl.rows);
+  const int kvh = unit % c.hkv, seq = unit / c.hkv;
+  if (seq >= c.n_seq) return;
+  const Tree tr = tree_of(c, t, seq);
+  const int group = t.hq / c.hkv;
+  const Parts pt = parts_of(tr, t.k_new != nullptr, P::KT, pl.splits);
+  if (r >= tr.n * group || pt.used == 1) return;
+  const int e = 4 * (threadIdx.x % (D / 4));
+  const int64_t base = (int64_t)unit * pl.splits * padded + r;
+  float big = neg_inf(), sum = 0.f;
+  f32x4 x = {};
+  for (int s = 0; s < pt.used; ++s)
+    big = fmaxf(big, t.pM[base + (int64_t)s * padded]);
+#pragma unroll 4
+  for (int s = 0; s < pt.used; ++s) {
+    const int64_t at = base + (int64_t)s * padded;
+    const float m = t.pM[at];
+    const float f = m == neg_inf() ? 0.f : exp2_(m - big);
+    sum += f * t.pL[at];
+    x += f * *(const f32x4*)(t.pO + at * D + e);
+  }
+  x *= sum == 0.f ? 0.f : 1.f / sum;
+  const int tok = r / group, h = kvh * group + r % group;
+  char* dst = t.out + (((int64_t)(tr.first + tok) * t.hq + h) * D + e) * P::ES;
+  if (P::ES == 2)
+    *(bf16x4*)dst = __builtin_convertvector(x, bf16x4);
+  else
+    *(f32x4*)dst = x;
+  if (t.lse && e == 0)
+    t.lse[(int64_t)h * t.n_tok + tr.first + tok] =
+        sum == 0.f ? neg_inf() : (big + log2_(sum)) * kLn2;
+}
+
+template <class P, int D>
+__global__ __launch_bounds__(kThreads) void join_kernel(const CacheView c,
+                                                        const TreePlan pl,
+                                                        const TreeCall t) {
+  join_rows<P, D>(c, pl, t,
+                  (int64_t)blockIdx.x * (kThreads / (D / 4)) +
+                      threadIdx.x / (D / 4));
+}
+
+// What a key's weight becomes.
+__device__ __forceinline__ void add_weight(const CacheView& c,
+                                           const TreeCall& t, const Tree& tr,
+                                           int unit, int key, float mass) {
+  if (key < tr.len) {
+    float* w = c.weight + (int64_t)unit * c.cap + key;
+    *w = t.decay * *w + mass;
+  }
+}
+
+// Few rows (16 at most): their logits were stored, four keys a thread here.
+constexpr int kStoredRows = 16;
+template <class P, int D>
+__global__ __launch_bounds__(kThreads) void mass_stored_kernel(
+    const CacheView c, const TreePlan pl, const TreeCall t, int join_blocks,
+    int key_blocks) {
+  if ((int)blockIdx.x < join_blocks) {
+    join_rows<P, D>(c, pl, t,
+                    (int64_t)blockIdx.x * (kThreads / (D / 4)) +
+                        threadIdx.x / (D / 4));
+    return;
+  }
+  __shared__ float lse2[kStoredRows], vote[kStoredRows];
+  const int b = blockIdx.x - join_blocks;
+  const int unit = b / key_blocks, kb = b % key_blocks;
+  const int kvh = unit % c.hkv, seq = unit / c.hkv;
+  const Tree tr = tree_of(c, t, seq);
+  if (tr.n == 0) return;
+  const int group = t.hq / c.hkv, n_rows = tr.n * group;
+  const Parts pt = parts_of(tr, t.k_new != nullptr, P::KT, pl.splits);
+  const int tid = threadIdx.x;
+  if (tid < n_rows) {
+    const int padded = pl.row_blocks * 16 * pl.row_tiles;
+    lse2[tid] = row_lse2(t, (int64_t)unit * pl.splits * padded + tid, padded,
+                         pt.used);
+    vote[tid] = t.vote ? t.vote[tr.first + tid / group] : 1.f;
+  }
+  __syncthreads();
+  const float* score =
+      t.score + (int64_t)unit * pl.rows * (pl.len_pad + kMaxTree);
+  auto sum = [&](int64_t at) {
+    f32x4 x[kStoredRows], acc = {};
+#pragma unroll
+    for (int r = 0; r < kStoredRows; ++r)
+      if (r < n_rows)
+        x[r] = *(const f32x4*)(score + r * (pl.len_pad + kMaxTree) + at);
+#pragma unroll
+    for (int r = 0; r < kStoredRows; ++r)
+      if (r < n_rows && vote[r] != 0.f && lse2[r] != neg_inf())
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          acc[i] += vote[r] * exp2_(x[r][i] - lse2[r]);
+    return acc;
+  };
+  const int64_t key = ((int64_t)kb * kThreads + tid) * 4;
+  if (key < tr.len) {
+    const f32x4 m = sum(key);
+    float* w = c.weight + (int64_t)unit * c.cap + key;
+    if (key + 4 <= tr.len) {
+      *(f32x4*)w = t.decay * *(const f32x4*)w + m;
+    } else {
+      for (int i = 0; key + i < tr.len; ++i) w[i] = t.decay * w[i] + m[i];
+    }
+  }
+  if (kb == 0 && t.w_new && 4 * tid < tr.n) {
+    if (!t.k_new) {
+      for (int i = 0; i < 4 && 4 * tid + i < tr.n; ++i)
+        t.w_new[(int64_t)(tr.first + 4 * tid + i) * c.hkv + kvh] = 0.f;
+    } else {
+      const f32x4 m = sum(pl.len_pad + 4 * tid);
+      for (int i = 0; i < 4 && 4 * tid + i < tr.n; ++i)
+        t.w_new[(int64_t)(tr.first + 4 * tid + i) * c.hkv + kvh] = m[i];
+    }
+  }
+}
+
+// Many rows: the logits are formed again, 16 NK keys a wavefront, whose rows
+// stay in registers while the query rows pass by.
+template <class P>
+constexpr int kMassHalves = P::ES == 2 ? 4 : 2;
+
+template <class P, int D>
+__global__ __launch_bounds__(kThreads) void mass_kernel(const CacheView c,
+                                                        const TreePlan pl,
+                                                        const TreeCall t,
+                                                        int key_blocks) {
+  constexpr int NK = kMassHalves<P>, TK = 16 * NK;
+  const int unit = blockIdx.x / key_blocks, kb = blockIdx.x % key_blocks;
+  const int kvh = unit % c.hkv, seq = unit / c.hkv;
+  const Tree tr = tree_of(c, t, seq);
+  if (tr.n == 0) return;
+  const int group = t.hq / c.hkv, n_rows = tr.n * group;
+  const Parts pt = parts_of(tr, t.k_new != nullptr, P::KT, pl.splits);
+  const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int cached = (tr.len + TK - 1) / TK;
+  const int tile = kb * kWaves + wave;
+  const bool draft = tile >= cached;
+  const int j0 = (tile - cached) * TK;
+  // (no barrier below: wavefronts without a tile leave)
+  if (draft && (j0 >= tr.n || !t.w_new)) return;
+  typename P::Row k[NK];
+  int n[NK];
+  uint64_t anc = 0;
+  if (!draft) {
+    Where<NK> at;
+    find<NK>(at, c, seq, kvh * c.head_bytes, tr.len, tile * TK);
+#pragma unroll
+    for (int h = 0; h < NK; ++h) {
+      P::load_row(k[h], c.k + at.off[h] + (uint32_t)c16 * c.token_bytes + 16 * g);
+      n[h] = at.n[h];
+    }
+  } else {
+    anc = ancestors(t, tr, lane);
+    const int64_t step = (int64_t)c.hkv * (D * P::ES);
+#pragma unroll
+    for (int h = 0; h < NK; ++h) {
+      n[h] = min(max(tr.n - j0 - 16 * h, 0), 16);
+      const int j = min(j0 + 16 * h + c16, tr.n - 1);
+      if (t.k_new)
+        P::load_row(k[h], t.k_new + (tr.first + j) * step + kvh * (D * P::ES) +
+                              16 * g);
+      else {
+        P::zero_row(k[h]);
+        n[h] = 0;
+      }
+    }
+  }
+  const int padded = pl.row_blocks * 16 * pl.row_tiles;
+  const int64_t base = (int64_t)unit * pl.splits * padded;
+  f32x4 acc[NK] = {};
+  for (int r0 = 0; r0 < n_rows; r0 += 16) {
+    const int r = min(r0 + c16, n_rows - 1), tok = r / group;
+    typename P::Row q;
+    P::load_row(q, t.q + ((int64_t)(tr.first + tok) * t.hq + kvh * group +
+                          r % group) * (D * P::ES) + 16 * g);
+    const float lse2 = row_lse2(t, base + r, padded, pt.used);
+    float vote = t.vote ? t.vote[tr.first + tok] : 1.f;
+    if (r0 + c16 >= n_rows || lse2 == neg_inf()) vote = 0.f;
+    const uint64_t sees = draft ? __shfl(anc, tok) >> j0 : 0;
+#pragma unroll
+    for (int h = 0; h < NK; ++h) {
+      const f32x4 x = P::qk(k[h], q);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bool see = !draft || (sees >> (16 * h + 4 * g + i) & 1);
+        if (vote != 0.f && see && 4 * g + i < n[h])
+          acc[h][i] += vote * exp2_(x[i] * t.scale_log2 - lse2);
+      }
+    }
+  }
+#pragma unroll
+  for (int h = 0; h < NK; ++h)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+      for (int o = 1; o < 16; o <<= 1) acc[h][i] += __shfl_xor(acc[h][i], o);
+      const int at = 16 * h + 4 * g + i;
+      if (c16 == 0) {
+        if (!draft)
+          add_weight(c, t, tr, unit, tile * TK + at, acc[h][i]);
+        else if (j0 + at < tr.n)
+          t.w_new[(int64_t)(tr.first + j0 + at) * c.hkv + kvh] = acc[h][i];
+      }
+    }
+}
+
+template <class P, int D>
+hipError_t launch_tree(const CacheView& c, const TreePlan& pl,
+                       const TreeCall& t, hipStream_t s) {
+  const int64_t units = (int64_t)c.n_seq * c.hkv * pl.splits;
+  const int64_t blocks = (units + 7) / 8 * 8 * pl.row_blocks;
+  if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)blocks), block(kThreads);
+  if (pl.stored)
+    tree_kernel<P, D, 1, true><<<grid, block, 0, s>>>(c, pl, t);
+  else if (pl.row_tiles == 1)
+    tree_kernel<P, D, 1, false><<<grid, block, 0, s>>>(c, pl, t);
+  else if (pl.row_tiles == 2)
+    tree_kernel<P, D, 2, false><<<grid, block, 0, s>>>(c, pl, t);
+  else if constexpr (P::ES == 2)
+    tree_kernel<P, D, 4, false><<<grid, block, 0, s>>>(c, pl, t);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  int64_t join = 0;
+  if (pl.splits > 1) {
+    constexpr int kRows = kThreads / (D / 4);
+    join = ((int64_t)c.n_seq * c.hkv * pl.rows + kRows - 1) / kRows;
+  }
+  if (pl.stored) {
+    const int kb = std::max(1, (t.max_len + 4 * kThreads - 1) / (4 * kThreads));
+    const int64_t n = join + (int64_t)c.n_seq * c.hkv * kb;
+    if (n > 0x7FFFFFFF) return hipErrorInvalidValue;
+    mass_stored_kernel<P, D><<<dim3((unsigned)n), block, 0, s>>>(
+        c, pl, t, (int)join, kb);
+    return hipGetLastError();
+  }
+  if (join) {
+    if (join > 0x7FFFFFFF) return hipErrorInvalidValue;
+    join_kernel<P, D><<<dim3((unsigned)join), block, 0, s>>>(c, pl, t);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (t.accumulate) {
+    constexpr int TK = 16 * kMassHalves<P>;
+    const int tiles = (t.max_len + TK - 1) / TK + (t.max_tree + TK - 1) / TK;
+    const int kb = (tiles + kWaves - 1) / kWaves;
+    const int64_t n = (int64_t)c.n_seq * c.hkv * kb;
+    if (n > 0x7FFFFFFF) return hipErrorInvalidValue;
+    mass_kernel<P, D><<<dim3((unsigned)n), block, 0, s>>>(c, pl, t, kb);
+    return hipGetLastError();
+  }
+  return hipSuccess;
+}
+
+}  // namespace
+
+TreePlan plan_tree(const CacheView& c, int32_t hq, int32_t max_tree,
+                   int32_t max_len, int32_t accumulate) {
+  TreePlan p{};
+  const int kt = c.fp32 ? 16 : 32;
+  p.rows = hq / c.hkv * max_tree;
+  p.row_tiles = p.rows <= 16 ? 1 : p.rows <= 32 || c.fp32 ? 2 : 4;
+  p.row_blocks = (p.rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles);
+  const int64_t tiles =
+      ((int64_t)max_len + kt - 1) / kt + (max_tree + kt - 1) / kt;
+  // about 2,048 work-groups for the 256 CUs, each with kMinTiles at least
+  const int64_t units = (int64_t)c.n_seq * c.hkv * p.row_blocks;
+  int64_t splits = std::max<int64_t>(1, 2048 / units);
+  splits = std::min(splits, (tiles + kMinTiles - 1) / kMinTiles);
+  p.splits = (int32_t)std::max<int64_t>(1, splits);
+  p.stored = accumulate && p.rows <= kStoredRows;
+  p.len_pad = ((int64_t)max_len + 31) / 32 * 32;
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = off;
+    off += (bytes + 255) & ~size_t(255);
+    return at;
+  };
+  const size_t part = (size_t)c.n_seq * c.hkv * p.splits * p.row_blocks * 16 *
+                      p.row_tiles;
+  p.pO = take(p.splits > 1 ? part * c.d * 4 : 0);
+  p.pM = take(p.splits > 1 || accumulate ? part * 4 : 0);
+  p.pL = take(p.splits > 1 || accumulate ? part * 4 : 0);
+  p.score = take(p.stored ? (size_t)c.n_seq * c.hkv * p.rows *
+                                (p.len_pad + kMaxTree) * 4
+                          : 0);
+  p.total = off;
+  return p;
+}
+
+hipError_t launch_tree_attention(const CacheView& c, const TreePlan& p,
+                                 const TreeCall& t, hipStream_t s) {
+  if (c.fp32)
+    return c.d == 64 ? launch_tree<TreeF32<64>, 64>(c, p, t, s)
+                     : launch_tree<TreeF32<128>, 128>(c, p, t, s);
+  return c.d == 64 ? launch_tree<TreeBf16<64>, 64>(c, p, t, s)
+                   : launch_tree<TreeBf16<128>, 128>(c, p, t, s);
+}
+
+}  // namespace evisel
