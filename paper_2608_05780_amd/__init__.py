@@ -421,19 +421,17 @@ def frame_evidence(mask: Mask, evidence, n_layers: int, e_qf,
         _stream(stream)))
 
 
-def _want(name, t, dtype, *shape):
-    """A dense tensor of this type on the current device, with at least these
-    axes (None: any size)."""
-    import torch
-    if t.dtype != dtype:
+def _want(name, t, dtype, shape, dev):
+    """A dense tensor of this type and shape (None: any) on device ``dev``."""
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
-    if t.dim() != len(shape) or any(
-            s is not None and s != g for s, g in zip(shape, t.shape)):
+    if t.shape != shape and shape is not None:
         raise ValueError(f"{name} has the shape {tuple(t.shape)}, not {shape}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    if t.is_cuda and t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} is not on the current device")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is not on the cache's device")
+    return t.data_ptr()
 
 
 class Cache:
@@ -454,39 +452,41 @@ class Cache:
                              "in shape, strides, type and device")
         if k.stride(3) != 1:
             raise ValueError("the last axis of k and v must be contiguous")
-        if k.is_cuda and k.device.index != torch.cuda.current_device():
-            raise ValueError("the cache is not on the current device")
+        if page_table.dim() != 2:
+            raise ValueError("page_table must be [n_seq, max_pages]")
         n_pages, page, hkv, d = k.shape
-        i32 = torch.int32
-        _want("page_table", page_table, i32, None, None)
         n_seq, max_pages = page_table.shape
-        _want("length", length, i32, n_seq)
-        if seen is not None:
-            _want("seen", seen, i32, n_seq)
-        if weight is not None:
-            _want("weight", weight, torch.float32, n_seq, hkv,
-                  max_pages * page)
-        if pos is not None:
-            _want("pos", pos, i32, n_seq, hkv, max_pages * page)
+        i32, dev = torch.int32, k.get_device()
+        slots = (n_seq, hkv, max_pages * page)
         self.k, self.v, self.page_table, self.length = k, v, page_table, length
         self.seen, self.weight, self.pos = seen, weight, pos
         self.n_seq, self.hkv, self.d, self.page = n_seq, hkv, d, page
         self.capacity = max_pages * page
-        p = lambda t: None if t is None else t.data_ptr()
+        self.dtype, self.device_index = k.dtype, dev
         # the stride of an axis of one is anything: a valid one instead
         ts = k.stride(1)
         hs = k.stride(2) if hkv > 1 else d
         ps = k.stride(0) if n_pages > 1 else max(page * ts, hkv * hs)
-        self._view = _CacheView(p(k), p(v), p(page_table), p(length), p(seen),
-                                p(weight), p(pos), n_pages, ps, ts, hs, n_seq,
-                                hkv, d, page, max_pages, _dtype_code(k))
+        self._view = _CacheView(
+            k.data_ptr(), v.data_ptr(),
+            _want("page_table", page_table, i32, None, dev),
+            _want("length", length, i32, (n_seq,), dev),
+            None if seen is None else _want("seen", seen, i32, (n_seq,), dev),
+            None if weight is None else
+            _want("weight", weight, torch.float32, slots, dev),
+            None if pos is None else _want("pos", pos, i32, slots, dev),
+            n_pages, ps, ts, hs, n_seq, hkv, d, page, max_pages,
+            _dtype_code(k))
         self._ref = ctypes.byref(self._view)
 
-    def _new_tokens(self, k_new, v_new):
-        n = k_new.shape[0]
-        for name, t in (("k_new", k_new), ("v_new", v_new)):
-            _want(name, t, self.k.dtype, n, self.hkv, self.d)
-        return n
+    def _checks(self):
+        """The device of a call's tensors: the cache's, which must be current
+        (a cache in host memory passes: the library refuses what it must)."""
+        if self.device_index >= 0:
+            import torch
+            if torch.cuda.current_device() != self.device_index:
+                raise ValueError("the cache is not on the current device")
+        return self.device_index
 
 
 def cache_append(cache: Cache, k_new, v_new, tok_ptr, max_new: int,
@@ -497,17 +497,22 @@ def cache_append(cache: Cache, k_new, v_new, tok_ptr, max_new: int,
     [n_seq]) pick some, in order; at most ``max_new`` a sequence. ``w_new``
     [n_tok, Hkv] fp32: their first accumulated weights (default 0)."""
     import torch
-    n = cache._new_tokens(k_new, v_new)
-    _want("tok_ptr", tok_ptr, torch.int32, cache.n_seq + 1)
-    if accept is not None:
-        _want("accept", accept, torch.int32, n)
-    if n_accept is not None:
-        _want("n_accept", n_accept, torch.int32, cache.n_seq)
-    if w_new is not None:
-        _want("w_new", w_new, torch.float32, n, cache.hkv)
-    _check(load().evisel_cache_append(
-        cache._ref, _ptr(k_new), _ptr(v_new), n, _ptr(tok_ptr), _ptr(accept),
-        _ptr(n_accept), int(max_new), _ptr(w_new), _stream(stream)))
+    dev, i32 = cache._checks(), torch.int32
+    n = k_new.shape[0]
+    rows = (n, cache.hkv, cache.d)
+    st = (_lib or load()).evisel_cache_append(
+        cache._ref, _want("k_new", k_new, cache.dtype, rows, dev),
+        _want("v_new", v_new, cache.dtype, rows, dev), n,
+        _want("tok_ptr", tok_ptr, i32, (cache.n_seq + 1,), dev),
+        None if accept is None else _want("accept", accept, i32, (n,), dev),
+        None if n_accept is None else
+        _want("n_accept", n_accept, i32, (cache.n_seq,), dev),
+        int(max_new),
+        None if w_new is None else
+        _want("w_new", w_new, torch.float32, (n, cache.hkv), dev),
+        _stream(stream))
+    if st:
+        _check(st)
 
 
 def tree_attention_workspace(cache: Cache, hq: int, max_tree: int,
@@ -534,33 +539,42 @@ def tree_attention(cache: Cache, q, k_new, v_new, tree_ptr, out, workspace,
     the drafted tokens' own. ``workspace``: a uint8 tensor of
     tree_attention_workspace bytes."""
     import torch
+    dev, f32 = cache._checks(), torch.float32
+    if q.dim() != 3 or q.shape[2] != cache.d:
+        raise ValueError("q must be [n_tok, Hq, d] with the cache's d")
     n, hq, d = q.shape
-    _want("q", q, cache.k.dtype, None, None, cache.d)
-    _want("out", out, cache.k.dtype, n, hq, d)
     if (k_new is None) != (v_new is None):
         raise ValueError("k_new and v_new come together")
-    if k_new is not None and cache._new_tokens(k_new, v_new) != n:
-        raise ValueError("k_new needs one row per row of q")
-    _want("tree_ptr", tree_ptr, torch.int32, cache.n_seq + 1)
-    if parent is not None:
-        _want("parent", parent, torch.int32, n)
-    f32 = torch.float32
-    if lse is not None:
-        _want("lse", lse, f32, hq, n)
-    if vote is not None:
-        _want("vote", vote, f32, n)
-    if w_new is not None:
-        _want("w_new", w_new, f32, n, cache.hkv)
     if decay is None and (vote is not None or w_new is not None):
         raise ValueError("vote and w_new need decay")
-    scale = float(softmax_scale) if softmax_scale is not None else d ** -0.5
-    _check(load().evisel_tree_attention(
-        cache._ref, hq, _ptr(q), _ptr(k_new), _ptr(v_new), n, _ptr(tree_ptr),
-        _ptr(parent), int(max_tree), int(max_len), scale, _ptr(out),
-        _ptr(lse), int(decay is not None), _ptr(vote),
-        0.0 if decay is None else float(decay), _ptr(w_new), _ptr(workspace),
-        0 if workspace is None else workspace.numel() * workspace.element_size(),
-        _stream(stream)))
+    kp = vp = None
+    if k_new is not None:
+        rows = (n, cache.hkv, d)
+        kp = _want("k_new", k_new, cache.dtype, rows, dev)
+        vp = _want("v_new", v_new, cache.dtype, rows, dev)
+    st = (_lib or load()).evisel_tree_attention(
+        cache._ref, hq, _want("q", q, cache.dtype, None, dev), kp, vp, n,
+        _want("tree_ptr", tree_ptr, torch.int32, (cache.n_seq + 1,), dev),
+        None if parent is None else
+        _want("parent", parent, torch.int32, (n,), dev), int(max_tree),
+        int(max_len), d ** -0.5 if softmax_scale is None else softmax_scale,
+        _want("out", out, cache.dtype, q.shape, dev),
+        None if lse is None else _want("lse", lse, f32, (hq, n), dev),
+        decay is not None,
+        None if vote is None else _want("vote", vote, f32, (n,), dev),
+        0.0 if decay is None else decay,
+        None if w_new is None else
+        _want("w_new", w_new, f32, (n, cache.hkv), dev),
+        *_scratch(workspace, dev), _stream(stream))
+    if st:
+        _check(st)
+
+
+def _scratch(workspace, dev):
+    if workspace is None:
+        return None, 0
+    return (_want("workspace", workspace, workspace.dtype, None, dev),
+            workspace.nbytes)
 
 
 def cache_evict_workspace(cache: Cache, budget: int, max_len: int) -> int:
@@ -576,11 +590,13 @@ def cache_evict(cache: Cache, budget: int, workspace, n_sink: int = 0,
     ``n_sink``, its last ``n_recent``, and the largest accumulated weights.
     No sequence has more than ``max_len`` tokens (default: the capacity).
     ``workspace``: a uint8 tensor of cache_evict_workspace bytes."""
-    _check(load().evisel_cache_evict(
+    dev = cache._checks()
+    st = (_lib or load()).evisel_cache_evict(
         cache._ref, int(budget), int(n_sink), int(n_recent),
-        cache.capacity if max_len is None else int(max_len), _ptr(workspace),
-        0 if workspace is None else workspace.numel() * workspace.element_size(),
-        _stream(stream)))
+        cache.capacity if max_len is None else int(max_len),
+        *_scratch(workspace, dev), _stream(stream))
+    if st:
+        _check(st)
 
 
 def profile_begin(capacity: int, all_kernels: bool = True, stride: int = 1):

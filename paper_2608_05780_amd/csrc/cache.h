@@ -70,6 +70,13 @@ struct EvictCall {
 hipError_t launch_cache_evict(const CacheView& c, const EvictCall& e,
                               hipStream_t s);
 
+// A row's reference moves when a logit passes it by this (log2 units): the
+// probabilities stay below 2^8, and fp32 sums and bf16 probabilities keep
+// their relative precision at any such scale. References and logits are kept
+// as q.k and scaled after their difference is taken, so that the keys that
+// matter, near the reference, carry no rounding of the scaled logit.
+constexpr float kTreeSlack = 8.0f;
+
 // How a tree attention call is split (host, from its bounds alone).
 struct TreePlan {
   int32_t rows;        // most query rows of a kv head: group * max_tree
@@ -79,7 +86,7 @@ struct TreePlan {
   int32_t stored;      // accumulate: the scores pass through the workspace
   int64_t len_pad;     // max_len rounded up, of the stored scores
   // workspace offsets and total, bytes
-  size_t pO, pM, pL, score, total;
+  size_t pO, pM, pL, row_m, row_inv, score, total;
 };
 
 struct TreeCall {
@@ -92,12 +99,26 @@ struct TreeCall {
   float* lse;                // may be null
   const float* vote;         // may be null
   float* w_new;              // may be null
-  float scale_log2, decay;
+  float scale, scale_log2;   // of the logits, and times log2(e)
+  float slack;               // how far (in q.k) a logit may pass a reference
+  float decay;
   int32_t hq, n_tok, max_tree, max_len, accumulate;
   float* pO;                 // [seq][kv head][split][row][d]
-  float* pM;                 // [seq][kv head][split][row], log2 units
-  float* pL;
-  float* score;              // [seq][kv head][row][len_pad + 64], log2 units
+  float* pM;                 // [seq][kv head][split][row] reference, as q.k
+  float* pL;                 //                            and sum
+  float* row_m;              // [seq][kv head][row] the same, over the splits:
+  float* row_inv;            // reference and 1 / sum (accumulate)
+  float* score;              // [seq][kv head][row][len_pad + 64] q.k
+
+  // exp(scale * x), x the difference of two q.k
+  __device__ __forceinline__ float exp_of(float x) const {
+    return __builtin_amdgcn_exp2f(x * scale_log2);
+  }
+  __device__ __forceinline__ float lse_of(float m, float sum) const {
+    return sum == 0.f ? -__builtin_inff()
+                      : m * scale + __builtin_amdgcn_logf(sum) *
+                                        0.69314718055994530942f;
+  }
 };
 TreePlan plan_tree(const CacheView& c, int32_t hq, int32_t max_tree,
                    int32_t max_len, int32_t accumulate);

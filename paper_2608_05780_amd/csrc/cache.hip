@@ -10,6 +10,7 @@ namespace {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // ---------------------------------------------------------------------------
 // Append.
@@ -170,24 +171,31 @@ __device__ __forceinline__ uint32_t keep_key(float w, int pos, int n_sink,
 constexpr int kEvThreads = 1024;
 constexpr int kEvWaves = kEvThreads / 64;
 constexpr int kEvBins = 2048;
-// keys that stay in LDS (the kernel's other arrays take 9 KB of the 160)
-constexpr int kEvLdsKeys = 36 * 1024;
+// keys that stay in LDS (the kernel's other arrays take 25 KB of the 160)
+constexpr int kEvLdsKeys = 32 * 1024;
+
+// keys of one digit's bin that stay in LDS as a list
+constexpr int kEvList = 4096;
 
 // One work-group per sequence and kv head: which slots it keeps, and from
 // that the moves. The budget-th largest key comes digit by digit (11, 11 and
-// 10 bits, a histogram each); equal keys are kept from the lowest slot on.
-// Then every wavefront walks its own run of slots twice: counting, and, with
-// what the runs before it counted, writing the holes below the budget and the
-// kept slots above it into the two lists. LDS: the keys stay in LDS between
-// the passes; otherwise each pass makes them again from weight and pos.
+// 10 bits, a histogram each): the first digit from every key, the others, as a
+// rule, from the short list of keys that share the digits before; equal keys
+// are kept from the lowest slot on. Then every wavefront walks its own run of
+// slots twice, 256 at a time: counting, and, with what the runs before it
+// counted, writing the holes below the budget and the kept slots above it into
+// the two lists. LDS: the keys stay in LDS between the passes; otherwise each
+// pass makes them again from weight and pos.
 template <bool LDS>
 __global__ __launch_bounds__(kEvThreads) void evict_select_kernel(
     const CacheView c, const EvictCall e) {
   __shared__ uint32_t hist[kEvBins];
+  __shared__ uint32_t list[kEvList];
   __shared__ uint32_t wave_tot[kEvWaves];
   __shared__ uint32_t found[2];          // the digit, and what is above it
+  __shared__ uint32_t listed;
   __shared__ int runs[kEvWaves][4];      // above / equal, below / from budget
-  extern __shared__ uint32_t keys[];
+  extern __shared__ __attribute__((aligned(16))) uint32_t keys[];
   const int unit = blockIdx.x, seq = unit / c.hkv;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -199,48 +207,41 @@ __global__ __launch_bounds__(kEvThreads) void evict_select_kernel(
   const int64_t recent_from = (int64_t)c.seen[seq] - e.n_recent;
   const float* w = c.weight + (int64_t)unit * c.cap;
   const int32_t* pos = c.pos + (int64_t)unit * c.cap;
+  // Keys i .. i + 3 (i a multiple of 4; the capacity is one of 16, so that
+  // slots past the length can be read). Which of them are there: i + u < len.
   auto make = [&](int i) {
-    return keep_key(w[i], pos[i], e.n_sink, recent_from);
-  };
-  if (LDS) {
-    for (int i = 4 * tid; i < len; i += 4 * kEvThreads) {
-      if (i + 4 <= len) {
-        const f32x4 x = *(const f32x4*)(w + i);
-        const i32x4 p = *(const i32x4*)(pos + i);
+    const f32x4 x = *(const f32x4*)(w + i);
+    const i32x4 p = *(const i32x4*)(pos + i);
+    u32x4 k;
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-          keys[i + u] = keep_key(x[u], p[u], e.n_sink, recent_from);
-      } else {
-        for (int u = 0; i + u < len; ++u) keys[i + u] = make(i + u);
-      }
-    }
-  }
-  auto key = [&](int i) { return LDS ? keys[i] : make(i); };
-
-  uint32_t prefix = 0, mask = 0;
-  uint32_t need = (uint32_t)e.budget;   // keys still wanted among the matching
-  for (int shift = 21; ; shift = shift == 21 ? 10 : 0) {
-    const int bits = shift ? 11 : 10;
+    for (int u = 0; u < 4; ++u)
+      k[u] = keep_key(x[u], p[u], e.n_sink, recent_from);
+    return k;
+  };
+  auto four = [&](int i) {
+    return LDS ? *(const u32x4*)(keys + i) : make(i);
+  };
+  // One key a lane into the histogram. The bin of the first lane that has one
+  // is added at once, so that a run of equal weights is no chain of additions
+  // to one place.
+  auto count = [&](bool in, uint32_t bin) {
+    const uint64_t active = __ballot(in);
+    if (!active) return;
+    const int lead = __builtin_ctzll(active);
+    const uint32_t b0 = __builtin_amdgcn_readlane(bin, lead);
+    const uint64_t same = __ballot(in && bin == b0);
+    if (lane == lead) atomicAdd(&hist[b0], (uint32_t)__popcll(same));
+    if (in && bin != b0) atomicAdd(&hist[bin], 1u);
+  };
+  auto clear = [&] {
     for (int i = tid; i < kEvBins; i += kEvThreads) hist[i] = 0;
+    if (tid == 0) listed = 0;
     __syncthreads();
-    for (int i0 = 0; i0 < len; i0 += kEvThreads) {
-      const int i = i0 + tid;
-      const uint32_t k = i < len ? key(i) : 0u;
-      const bool in = i < len && (k & mask) == prefix;
-      const uint32_t bin = (k >> shift) & ((1u << bits) - 1);
-      const uint64_t active = __ballot(in);
-      if (!active) continue;
-      // the bin of the first lane is added at once, so that a run of equal
-      // weights is no chain of additions to one place
-      const int lead = __builtin_ctzll(active);
-      const uint32_t b0 = __builtin_amdgcn_readlane(bin, lead);
-      const uint64_t same = __ballot(in && bin == b0);
-      if (lane == lead) atomicAdd(&hist[b0], (uint32_t)__popcll(same));
-      if (in && bin != b0) atomicAdd(&hist[bin], 1u);
-    }
+  };
+  // The bin, from the largest down, in which the running count reaches
+  // `need`: found[0], and the count above it: found[1]. Two bins a thread.
+  auto locate = [&](uint32_t need) {
     __syncthreads();
-    // bins from the largest down, two per thread: the one in which the
-    // running count reaches `need`
     const uint32_t c0 = hist[kEvBins - 1 - 2 * tid];
     const uint32_t c1 = hist[kEvBins - 2 - 2 * tid];
     uint32_t run = c0 + c1;
@@ -261,27 +262,98 @@ __global__ __launch_bounds__(kEvThreads) void evict_select_kernel(
       found[1] = before + c0;
     }
     __syncthreads();
-    prefix |= found[0] << shift;
-    mask |= ((1u << bits) - 1) << shift;
-    need -= found[1];
-    if (shift == 0) break;
+  };
+  constexpr int kStep = 4 * kEvThreads;
+
+  // first digit
+  clear();
+#pragma unroll 2
+  for (int i0 = 0; i0 < len; i0 += kStep) {
+    const int i = i0 + 4 * tid;
+    u32x4 k = {};
+    if (i < len) {
+      k = make(i);
+      if (LDS) *(u32x4*)(keys + i) = k;
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) count(i + u < len, k[u] >> 21);
   }
+  uint32_t need = (uint32_t)e.budget;   // keys still wanted among the matching
+  locate(need);
+  uint32_t prefix = found[0] << 21;
+  need -= found[1];
+  // the keys that share it, into the list (or, if they are too many, again
+  // from all keys), and their second digit
+  clear();
+#pragma unroll 2
+  for (int i0 = 0; i0 < len; i0 += kStep) {
+    const int i = i0 + 4 * tid;
+    u32x4 k = {};
+    if (i < len) k = four(i);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const bool in = i + u < len && (k[u] & 0xFFE00000u) == prefix;
+      const uint64_t m = __ballot(in);
+      if (!m) continue;
+      const int lead = __builtin_ctzll(m);
+      uint32_t at = 0;
+      if (lane == lead) at = atomicAdd(&listed, (uint32_t)__popcll(m));
+      at = __builtin_amdgcn_readlane(at, lead) +
+           (uint32_t)__popcll(m & ((1ull << lane) - 1));
+      if (in && at < kEvList) list[at] = k[u];
+      count(in, (k[u] >> 10) & 2047u);
+    }
+  }
+  locate(need);
+  prefix |= found[0] << 10;
+  need -= found[1];
+  const uint32_t n_list = listed;
+  __syncthreads();   // every thread has read `listed`
+  clear();
+  if (n_list <= kEvList) {
+    for (uint32_t i0 = 0; i0 < n_list; i0 += kEvThreads) {
+      const uint32_t i = i0 + tid, k = i < n_list ? list[i] : 0u;
+      count(i < n_list && (k & 0xFFFFFC00u) == prefix, k & 1023u);
+    }
+  } else {
+    for (int i0 = 0; i0 < len; i0 += kStep) {
+      const int i = i0 + 4 * tid;
+      u32x4 k = {};
+      if (i < len) k = four(i);
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        count(i + u < len && (k[u] & 0xFFFFFC00u) == prefix, k[u] & 1023u);
+    }
+  }
+  locate(need);
+  prefix |= found[0];
+  need -= found[1];
   // kept: keys above `prefix`, and the first `need` that equal it
 
-  const int per = ((len + 64 * kEvWaves - 1) / (64 * kEvWaves)) * 64;
+  const int per = ((len + 256 * kEvWaves - 1) / (256 * kEvWaves)) * 256;
   const int a = min(wave * per, len), b = min(a + per, len);
   int n_gt[2] = {0, 0}, n_eq[2] = {0, 0};
-  for (int i0 = a; i0 < b; i0 += 64) {
-    const int i = i0 + lane;
-    const bool in = i < b, hi = i >= e.budget;
-    const uint32_t k = in ? key(i) : 0u;
-    const uint64_t gt = __ballot(in && k > prefix);
-    const uint64_t eq = __ballot(in && k == prefix);
-    const uint64_t top = __ballot(hi);
-    n_gt[0] += __popcll(gt & ~top);
-    n_gt[1] += __popcll(gt & top);
-    n_eq[0] += __popcll(eq & ~top);
-    n_eq[1] += __popcll(eq & top);
+#pragma unroll 2
+  for (int i0 = a; i0 < b; i0 += 256) {
+    const int i = i0 + 4 * lane;
+    u32x4 k = {};
+    if (i < b) k = four(i);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const bool in = i + u < b, hi = i + u >= e.budget;
+      const bool gt = in && k[u] > prefix, eq = in && k[u] == prefix;
+      n_gt[0] += gt && !hi;
+      n_gt[1] += gt && hi;
+      n_eq[0] += eq && !hi;
+      n_eq[1] += eq && hi;
+    }
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    n_gt[0] += __shfl_xor(n_gt[0], o);
+    n_gt[1] += __shfl_xor(n_gt[1], o);
+    n_eq[0] += __shfl_xor(n_eq[0], o);
+    n_eq[1] += __shfl_xor(n_eq[1], o);
   }
   if (lane == 0) {
     runs[wave][0] = n_gt[0];
@@ -304,22 +376,45 @@ __global__ __launch_bounds__(kEvThreads) void evict_select_kernel(
   }
   int32_t* to = e.to + (int64_t)unit * e.max_moves;
   int32_t* from = e.from + (int64_t)unit * e.max_moves;
-  for (int i0 = a; i0 < b; i0 += 64) {
-    const int i = i0 + lane;
-    const bool in = i < b, hi = i >= e.budget;
-    const uint32_t k = in ? key(i) : 0u;
-    const uint64_t below_lane = (1ull << lane) - 1;
-    const uint64_t eq = __ballot(in && k == prefix);
-    const bool kept =
-        in && (k > prefix ||
-               (k == prefix && eqs + __popcll(eq & below_lane) < (int)need));
-    eqs += __popcll(eq);
-    const uint64_t hole = __ballot(in && !hi && !kept);
-    const uint64_t tail = __ballot(in && hi && kept);
-    if (in && !hi && !kept) to[holes + __popcll(hole & below_lane)] = i;
-    if (in && hi && kept) from[tails + __popcll(tail & below_lane)] = i;
-    holes += __popcll(hole);
-    tails += __popcll(tail);
+  const uint64_t below_lane = (1ull << lane) - 1;
+#pragma unroll 2
+  for (int i0 = a; i0 < b; i0 += 256) {
+    const int i = i0 + 4 * lane;
+    u32x4 k = {};
+    if (i < b) k = four(i);
+    // slots in order: lane by lane, each its four
+    int before = eqs;
+    bool eq[4], kept[4], out[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      eq[u] = i + u < b && k[u] == prefix;
+      const uint64_t m = __ballot(eq[u]);
+      before += __popcll(m & below_lane);
+      eqs += __popcll(m);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      kept[u] = i + u < b &&
+                (k[u] > prefix || (eq[u] && before < (int)need));
+      before += eq[u];
+    }
+    int hole = holes, tail = tails;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const bool hi = i + u >= e.budget;
+      out[u] = i + u < b && !hi && !kept[u];
+      kept[u] = kept[u] && hi;
+      const uint64_t mh = __ballot(out[u]), mt = __ballot(kept[u]);
+      hole += __popcll(mh & below_lane);
+      tail += __popcll(mt & below_lane);
+      holes += __popcll(mh);
+      tails += __popcll(mt);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (out[u]) to[hole++] = i + u;
+      if (kept[u]) from[tail++] = i + u;
+    }
   }
   if (wave == kEvWaves - 1 && lane == 0) e.count[unit] = tails;
 }
@@ -388,7 +483,7 @@ hipError_t launch_cache_evict(const CacheView& c, const EvictCall& e,
   if ((int64_t)c.n_seq * c.hkv > 0x7FFFFFFF) return hipErrorInvalidValue;
   if (e.max_len <= kEvLdsKeys) {
     const size_t lds = ((size_t)e.max_len * 4 + 15) & ~size_t(15);
-    if (lds + 16 * 1024 > 64 * 1024) {
+    if (lds + 32 * 1024 > 64 * 1024) {
       const hipError_t r = hipFuncSetAttribute(
           (const void*)evict_select_kernel<true>,
           hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);

@@ -190,7 +190,9 @@ evisel_status evisel_tree_attention(
   t.lse = lse;
   t.vote = accumulate ? vote : nullptr;
   t.w_new = accumulate ? w_new : nullptr;
+  t.scale = softmax_scale;
   t.scale_log2 = softmax_scale * 1.4426950408889634f;
+  t.slack = std::min(evisel::kTreeSlack / t.scale_log2, 1e30f);
   t.decay = decay;
   t.hq = hq;
   t.n_tok = n_tok;
@@ -201,6 +203,8 @@ evisel_status evisel_tree_attention(
   t.pO = (float*)(w + p.pO);
   t.pM = (float*)(w + p.pM);
   t.pL = (float*)(w + p.pL);
+  t.row_m = (float*)(w + p.row_m);
+  t.row_inv = (float*)(w + p.row_inv);
   t.score = (float*)(w + p.score);
   const hipError_t e =
       evisel::launch_tree_attention(c, p, t, (hipStream_t)stream);

@@ -14,24 +14,13 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kWaves = 4;
-constexpr int kThreads = 64 * kWaves;
+constexpr int kThreads = 256;   // of the kernels behind the attention itself
 constexpr int kMaxTree = 64;
-constexpr float kLn2 = 0.69314718055994530942f;
-// A row's reference moves when a logit passes it by this (log2 units): the
-// probabilities stay below 2^8, and fp32 sums and bf16 probabilities keep
-// their relative precision at any such scale.
-constexpr float kSlack = 8.0f;
-// Key tiles a split has at least.
-constexpr int kMinTiles = 4;
+constexpr int kMaxSplits = 128;
+// Wavefronts of a work-group that takes 16 RT rows.
+constexpr int waves_of(int row_tiles) { return row_tiles == 4 ? 4 : 8; }
 
 __device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
-__device__ __forceinline__ float exp2_(float x) {
-  return __builtin_amdgcn_exp2f(x);
-}
-__device__ __forceinline__ float log2_(float x) {
-  return __builtin_amdgcn_logf(x);
-}
 // Over the four lanes that hold one query row (lane % 16).
 __device__ __forceinline__ float row_max(float x) {
   x = fmaxf(x, __shfl_xor(x, 16));
@@ -135,12 +124,13 @@ struct TreeBf16 {
   static __device__ float element(const char* row, int e) {
     return __uint_as_float((uint32_t)((const uint16_t*)row)[e] << 16);
   }
-  static __device__ void store(char* dst, const float (&x)[D / 16]) {
-    typedef __bf16 out_t __attribute__((ext_vector_type(D / 16)));
-    typedef float in_t __attribute__((ext_vector_type(D / 16)));
+  template <int N>
+  static __device__ void store(char* dst, const float (&x)[N]) {
+    typedef __bf16 out_t __attribute__((ext_vector_type(N)));
+    typedef float in_t __attribute__((ext_vector_type(N)));
     in_t v;
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) v[i] = x[i];
+    for (int i = 0; i < N; ++i) v[i] = x[i];
     *(out_t*)dst = __builtin_convertvector(v, out_t);
   }
 };
@@ -216,12 +206,10 @@ struct TreeF32 {
   static __device__ float element(const char* row, int e) {
     return ((const float*)row)[e];
   }
-  static __device__ void store(char* dst, const float (&x)[D / 16]) {
+  template <int N>
+  static __device__ void store(char* dst, const float (&x)[N]) {
 #pragma unroll
-    for (int i = 0; i < D / 16; i += 4) {
-      const f32x4 v = {x[i], x[i + 1], x[i + 2], x[i + 3]};
-      *(f32x4*)(dst + 4 * i) = v;
-    }
+    for (int i = 0; i < N; ++i) ((float*)dst)[i] = x[i];
   }
 };
 
@@ -260,7 +248,7 @@ __device__ __forceinline__ Parts parts_of(const Tree& r, bool drafts, int kt,
   Parts p;
   p.cached = (r.len + kt - 1) / kt;
   p.total = p.cached + (drafts ? (r.n + kt - 1) / kt : 0);
-  p.per = max((p.total + splits - 1) / splits, kMinTiles);
+  p.per = max((p.total + splits - 1) / splits, 1);
   p.used = max((p.total + p.per - 1) / p.per, 1);
   return p;
 }
@@ -332,19 +320,16 @@ template <class P, int D, int RT>
 struct Rows {
   typename P::Row q[RT];
   f32x4 o[RT][P::NT];
-  float m[RT], l[RT];   // reference and sum, log2 units
+  float m[RT], l[RT];   // reference (q.k) and sum
 
-  // Logits of a tile of keys; score: where they go, or null. vis[rt]: bit
-  // 4h + i set if the row sees key 16h + 4g + i (all: every row sees every
-  // key).
   __device__ __forceinline__ void logits(f32x4 (&x)[RT][P::NH],
-                                         const typename P::Row (&k)[P::NH],
-                                         float scale) {
+                                         const typename P::Row (&k)[P::NH]) {
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-      for (int h = 0; h < P::NH; ++h) x[rt][h] = P::qk(k[h], q[rt]) * scale;
+      for (int h = 0; h < P::NH; ++h) x[rt][h] = P::qk(k[h], q[rt]);
   }
+  // vis[rt]: bit 4h + i set if the row sees key 16h + 4g + i.
   __device__ __forceinline__ static void hide(f32x4 (&x)[RT][P::NH],
                                               const uint32_t (&vis)[RT]) {
 #pragma unroll
@@ -356,7 +341,8 @@ struct Rows {
           if (!(vis[rt] >> (4 * h + i) & 1)) x[rt][h][i] = neg_inf();
   }
   // Logits to probabilities (against the rows' references) and their sums.
-  __device__ __forceinline__ void softmax(f32x4 (&x)[RT][P::NH]) {
+  __device__ __forceinline__ void softmax(f32x4 (&x)[RT][P::NH],
+                                          const TreeCall& t) {
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       float top = neg_inf();
@@ -364,20 +350,20 @@ struct Rows {
       for (int h = 0; h < P::NH; ++h)
 #pragma unroll
         for (int i = 0; i < 4; ++i) top = fmaxf(top, x[rt][h][i]);
-      if (__any(top > m[rt] + kSlack)) {
+      if (__any(top > m[rt] + t.slack)) {
         const float next = fmaxf(m[rt], row_max(top));
-        const float a = m[rt] == neg_inf() ? 0.f : exp2_(m[rt] - next);
+        const float a = m[rt] == neg_inf() ? 0.f : t.exp_of(m[rt] - next);
         m[rt] = next;
         l[rt] *= a;
 #pragma unroll
-        for (int t = 0; t < P::NT; ++t) o[rt][t] *= a;
+        for (int u = 0; u < P::NT; ++u) o[rt][u] *= a;
       }
       const float ref = m[rt] == neg_inf() ? 0.f : m[rt];
 #pragma unroll
       for (int h = 0; h < P::NH; ++h)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          x[rt][h][i] = exp2_(x[rt][h][i] - ref);
+          x[rt][h][i] = t.exp_of(x[rt][h][i] - ref);
           l[rt] += x[rt][h][i];
         }
     }
@@ -395,9 +381,9 @@ struct Rows {
 // joined in LDS at the end. What a run's rows come to is the output, if the
 // sequence has one run, or a partial sum in the workspace.
 template <class P, int D, int RT, bool SCORE>
-__global__ __launch_bounds__(kThreads, RT == 4 ? 1 : 2) void tree_kernel(
+__global__ __launch_bounds__(64 * waves_of(RT), RT == 4 ? 1 : 2) void tree_kernel(
     const CacheView c, const TreePlan pl, const TreeCall t) {
-  constexpr int KT = P::KT, NH = P::NH;
+  constexpr int KT = P::KT, NH = P::NH, kWaves = waves_of(RT);
   constexpr int kPad = D + 4;
   // a wavefront's share of one row tile's O, or its probabilities of a tile
   constexpr int kOwn = RT * KT > kPad ? 16 * RT * KT : 16 * kPad;
@@ -463,7 +449,7 @@ __global__ __launch_bounds__(kThreads, RT == 4 ? 1 : 2) void tree_kernel(
       constexpr bool kMore = decltype(more)::value;
       if (kMore) find<NH>(next, c, seq, head, end, (tile + kWaves) * KT);
       f32x4 x[RT][NH];
-      rows.logits(x, k, t.scale_log2);
+      rows.logits(x, k);
       if (kMore) fetch_k<P>(k, c, next, koff);
       bool full = true;
 #pragma unroll
@@ -489,7 +475,7 @@ __global__ __launch_bounds__(kThreads, RT == 4 ? 1 : 2) void tree_kernel(
 #pragma unroll
         for (int h = 0; h < NH; ++h)
           *(f32x4*)(score[0] + (int64_t)tile * KT + 16 * h) = x[0][h];
-      rows.softmax(x);
+      rows.softmax(x, t);
       typename P::ValT vt;
       P::turn(vt, v);
       if (kMore) fetch_v<P>(v, c, next, voff);
@@ -539,13 +525,13 @@ __global__ __launch_bounds__(kThreads, RT == 4 ? 1 : 2) void tree_kernel(
         vis[rt] |= (sees[rt] >> (16 * h + 4 * g) & 15u) << (4 * h);
     }
     f32x4 p[RT][NH];
-    rows.logits(p, x.k, t.scale_log2);
+    rows.logits(p, x.k);
     rows.hide(p, vis);
     if (SCORE && score[0])
 #pragma unroll
       for (int h = 0; h < NH; ++h)
         *(f32x4*)(score[0] + pl.len_pad + j0 + 16 * h) = p[0][h];
-    rows.softmax(p);
+    rows.softmax(p, t);
     // A value that is not finite reaches the rows that see its token and no
     // other: it is left out of the product, whose zeros it would spoil, and
     // added by itself.
@@ -586,7 +572,7 @@ __global__ __launch_bounds__(kThreads, RT == 4 ? 1 : 2) void tree_kernel(
     __builtin_amdgcn_wave_barrier();
   }
 
-  // the four wavefronts' rows
+  // the wavefronts' rows
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     rows.l[rt] = row_sum(rows.l[rt]);
@@ -596,16 +582,17 @@ __global__ __launch_bounds__(kThreads, RT == 4 ? 1 : 2) void tree_kernel(
     }
   }
   __syncthreads();
-  const int er = threadIdx.x / 16, ec = threadIdx.x % 16;   // row, columns
-  const int64_t part = ((int64_t)unit * pl.splits + split) *
-                       (pl.row_blocks * 16 * RT);
+  constexpr int kCols = 16 * D / (64 * kWaves);   // of a thread
+  const int er = threadIdx.x / (D / kCols), ec = threadIdx.x % (D / kCols);
+  const int padded = pl.row_blocks * 16 * RT;
+  const int64_t part = ((int64_t)unit * pl.splits + split) * padded;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     float top = neg_inf();
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sm[w][16 * rt + c16]);
     const float f =
-        rows.m[rt] == neg_inf() ? 0.f : exp2_(rows.m[rt] - top);
+        rows.m[rt] == neg_inf() ? 0.f : t.exp_of(rows.m[rt] - top);
 #pragma unroll
     for (int u = 0; u < P::NT; ++u)
 #pragma unroll
@@ -621,97 +608,117 @@ __global__ __launch_bounds__(kThreads, RT == 4 ? 1 : 2) void tree_kernel(
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
         const float mw = sm[w][16 * rt + er];
-        sum += (mw == neg_inf() ? 0.f : exp2_(mw - big)) * sl[w][16 * rt + er];
+        sum += (mw == neg_inf() ? 0.f : t.exp_of(mw - big)) *
+               sl[w][16 * rt + er];
       }
-      float x[D / 16] = {};
+      float x[kCols] = {};
 #pragma unroll
       for (int w = 0; w < kWaves; ++w)
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i)
-          x[i] += so[w][er * kPad + ec * (D / 16) + i];
+        for (int i = 0; i < kCols; ++i)
+          x[i] += so[w][er * kPad + ec * kCols + i];
       if (pt.used == 1) {
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) x[i] *= inv;
+        for (int i = 0; i < kCols; ++i) x[i] *= inv;
         const int tok = r / group, h = kvh * group + r % group;
-        P::store(t.out + ((int64_t)(tr.first + tok) * t.hq + h) * (D * P::ES) +
-                     ec * (D / 16) * P::ES, x);
-        if (t.lse && ec == 0)
-          t.lse[(int64_t)h * t.n_tok + tr.first + tok] =
-              sum == 0.f ? neg_inf() : (big + log2_(sum)) * kLn2;
+        P::template store<kCols>(
+            t.out + ((int64_t)(tr.first + tok) * t.hq + h) * (D * P::ES) +
+                ec * kCols * P::ES, x);
+        if (ec == 0) {
+          if (t.lse)
+            t.lse[(int64_t)h * t.n_tok + tr.first + tok] = t.lse_of(big, sum);
+          if (t.accumulate) {
+            t.row_m[(int64_t)unit * padded + r] = big;
+            t.row_inv[(int64_t)unit * padded + r] = inv;
+          }
+        }
       } else {
-        float* dst = t.pO + (part + r) * D + ec * (D / 16);
+        float* dst = t.pO + (part + r) * D + ec * kCols;
 #pragma unroll
-        for (int i = 0; i < D / 16; i += 4)
-          *(f32x4*)(dst + i) = f32x4{x[i], x[i + 1], x[i + 2], x[i + 3]};
-      }
-      if (ec == 0 && (pt.used > 1 || t.accumulate)) {
-        t.pM[part + r] = big;
-        t.pL[part + r] = sum;
+        for (int i = 0; i < kCols; ++i) dst[i] = x[i];
+        if (ec == 0) {
+          t.pM[part + r] = big;
+          t.pL[part + r] = sum;
+        }
       }
     }
     __syncthreads();
   }
 }
 
-// log2 of a row's whole sum, from its splits.
-__device__ __forceinline__ float row_lse2(const TreeCall& t, int64_t base,
-                                          int64_t stride, int used) {
-  float big = neg_inf(), sum = 0.f;
-  for (int s = 0; s < used; ++s) big = fmaxf(big, t.pM[base + s * stride]);
-  for (int s = 0; s < used; ++s) {
-    const float m = t.pM[base + s * stride];
-    sum += (m == neg_inf() ? 0.f : exp2_(m - big)) * t.pL[base + s * stride];
-  }
-  return sum == 0.f ? neg_inf() : big + log2_(sum);
-}
-
-// The splits of a row joined, D / 4 threads a row.
+// The join of row r over its sequence's splits, by a work-group: D / 4
+// threads a split, the splits in turn over the groups of D / 4 threads.
 template <class P, int D>
-__device__ __forceinline__ void join_rows(const CacheView& c,
-                                          const TreePlan& pl,
-                                          const TreeCall& t, int64_t row) {
+__device__ __forceinline__ void join_row(const CacheView& c,
+                                         const TreePlan& pl, const TreeCall& t,
+                                         int64_t row) {
+  constexpr int kLanes = D / 4, kGroups = kThreads / kLanes;
+  __shared__ __attribute__((aligned(16))) float part[kGroups][D];
+  __shared__ float part_l[kGroups];
   const int padded = pl.row_blocks * 16 * pl.row_tiles;
   const int unit = (int)(row / pl.rows), r = (int)(row % pl.rows);
   const int kvh = unit % c.hkv, seq = unit / c.hkv;
-  if (seq >= c.n_seq) return;
   const Tree tr = tree_of(c, t, seq);
   const int group = t.hq / c.hkv;
   const Parts pt = parts_of(tr, t.k_new != nullptr, P::KT, pl.splits);
   if (r >= tr.n * group || pt.used == 1) return;
-  const int e = 4 * (threadIdx.x % (D / 4));
   const int64_t base = (int64_t)unit * pl.splits * padded + r;
-  float big = neg_inf(), sum = 0.f;
+  const int lane = threadIdx.x & 63;
+  // every wavefront finds the largest reference for itself
+  float big = neg_inf();
+  static_assert(kMaxSplits <= 128, "two a lane");
+#pragma unroll
+  for (int u = 0; u < kMaxSplits / 64; ++u)
+    if (lane + 64 * u < pt.used)
+      big = fmaxf(big, t.pM[base + (int64_t)(lane + 64 * u) * padded]);
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) big = fmaxf(big, __shfl_xor(big, o));
+  const int e = 4 * (threadIdx.x % kLanes), gr = threadIdx.x / kLanes;
+  float sum = 0.f;
   f32x4 x = {};
-  for (int s = 0; s < pt.used; ++s)
-    big = fmaxf(big, t.pM[base + (int64_t)s * padded]);
 #pragma unroll 4
-  for (int s = 0; s < pt.used; ++s) {
+  for (int s = gr; s < pt.used; s += kGroups) {
     const int64_t at = base + (int64_t)s * padded;
-    const float m = t.pM[at];
-    const float f = m == neg_inf() ? 0.f : exp2_(m - big);
-    sum += f * t.pL[at];
-    x += f * *(const f32x4*)(t.pO + at * D + e);
+    const float m = t.pM[at], l = t.pL[at];
+    const f32x4 o = *(const f32x4*)(t.pO + at * D + e);
+    const float f = m == neg_inf() ? 0.f : t.exp_of(m - big);
+    sum += f * l;
+    x += f * o;
   }
-  x *= sum == 0.f ? 0.f : 1.f / sum;
+  *(f32x4*)&part[gr][e] = x;
+  if (e == 0) part_l[gr] = sum;
+  __syncthreads();
+  if (gr) return;
+  x = f32x4{};
+  sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < kGroups; ++i) {
+    x += *(const f32x4*)&part[i][e];
+    sum += part_l[i];
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  x *= inv;
   const int tok = r / group, h = kvh * group + r % group;
   char* dst = t.out + (((int64_t)(tr.first + tok) * t.hq + h) * D + e) * P::ES;
-  if (P::ES == 2)
+  if constexpr (P::ES == 2)
     *(bf16x4*)dst = __builtin_convertvector(x, bf16x4);
   else
     *(f32x4*)dst = x;
-  if (t.lse && e == 0)
-    t.lse[(int64_t)h * t.n_tok + tr.first + tok] =
-        sum == 0.f ? neg_inf() : (big + log2_(sum)) * kLn2;
+  if (e) return;
+  if (t.lse)
+    t.lse[(int64_t)h * t.n_tok + tr.first + tok] = t.lse_of(big, sum);
+  if (t.accumulate) {
+    t.row_m[(int64_t)unit * padded + r] = big;
+    t.row_inv[(int64_t)unit * padded + r] = inv;
+  }
 }
 
 template <class P, int D>
 __global__ __launch_bounds__(kThreads) void join_kernel(const CacheView c,
                                                         const TreePlan pl,
                                                         const TreeCall t) {
-  join_rows<P, D>(c, pl, t,
-                  (int64_t)blockIdx.x * (kThreads / (D / 4)) +
-                      threadIdx.x / (D / 4));
+  join_row<P, D>(c, pl, t, blockIdx.x);
 }
 
 // What a key's weight becomes.
@@ -725,31 +732,67 @@ __device__ __forceinline__ void add_weight(const CacheView& c,
 }
 
 // Few rows (16 at most): their logits were stored, four keys a thread here.
+// The same launch joins the rows; the weights' work-groups take the rows'
+// sums from the splits themselves.
 constexpr int kStoredRows = 16;
 template <class P, int D>
 __global__ __launch_bounds__(kThreads) void mass_stored_kernel(
     const CacheView c, const TreePlan pl, const TreeCall t, int join_blocks,
     int key_blocks) {
   if ((int)blockIdx.x < join_blocks) {
-    join_rows<P, D>(c, pl, t,
-                    (int64_t)blockIdx.x * (kThreads / (D / 4)) +
-                        threadIdx.x / (D / 4));
+    join_row<P, D>(c, pl, t, blockIdx.x);
     return;
   }
-  __shared__ float lse2[kStoredRows], vote[kStoredRows];
+  __shared__ float row_m[kStoredRows], coef[kStoredRows];
   const int b = blockIdx.x - join_blocks;
   const int unit = b / key_blocks, kb = b % key_blocks;
   const int kvh = unit % c.hkv, seq = unit / c.hkv;
   const Tree tr = tree_of(c, t, seq);
-  if (tr.n == 0) return;
+  const int64_t key0 = (int64_t)kb * kThreads * 4;
+  if (tr.n == 0 || (key0 >= tr.len && kb > 0)) return;
   const int group = t.hq / c.hkv, n_rows = tr.n * group;
   const Parts pt = parts_of(tr, t.k_new != nullptr, P::KT, pl.splits);
   const int tid = threadIdx.x;
-  if (tid < n_rows) {
-    const int padded = pl.row_blocks * 16 * pl.row_tiles;
-    lse2[tid] = row_lse2(t, (int64_t)unit * pl.splits * padded + tid, padded,
-                         pt.used);
-    vote[tid] = t.vote ? t.vote[tr.first + tid / group] : 1.f;
+  const int64_t key = key0 + 4 * tid;
+  const int padded = pl.row_blocks * 16 * pl.row_tiles;
+  // sixteen threads a row
+  {
+    const int r = tid / 16, l16 = tid % 16;
+    float m = neg_inf(), cf = 0.f;
+    if (r < n_rows) {
+      if (pt.used == 1) {
+        m = t.row_m[(int64_t)unit * padded + r];
+        cf = t.row_inv[(int64_t)unit * padded + r];
+      } else {
+        const int64_t base = (int64_t)unit * pl.splits * padded + r;
+        float pm[kMaxSplits / 16], sum = 0.f;
+#pragma unroll
+        for (int u = 0; u < kMaxSplits / 16; ++u) {
+          const int s = l16 + 16 * u;
+          pm[u] = s < pt.used ? t.pM[base + (int64_t)s * padded] : neg_inf();
+          m = fmaxf(m, pm[u]);
+        }
+#pragma unroll
+        for (int o = 1; o < 16; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
+#pragma unroll
+        for (int u = 0; u < kMaxSplits / 16; ++u) {
+          const int s = l16 + 16 * u;
+          if (s < pt.used)
+            sum += (pm[u] == neg_inf() ? 0.f : t.exp_of(pm[u] - m)) *
+                   t.pL[base + (int64_t)s * padded];
+        }
+#pragma unroll
+        for (int o = 1; o < 16; o <<= 1) sum += __shfl_xor(sum, o);
+        cf = sum == 0.f ? 0.f : 1.f / sum;
+      }
+      const float vote = t.vote ? t.vote[tr.first + r / group] : 1.f;
+      // (a vote of 0 keeps the row out, whatever it holds)
+      cf = vote == 0.f ? 0.f : cf * vote;
+    }
+    if (l16 == 0) {
+      row_m[r] = m;
+      coef[r] = cf;
+    }
   }
   __syncthreads();
   const float* score =
@@ -762,13 +805,12 @@ __global__ __launch_bounds__(kThreads) void mass_stored_kernel(
         x[r] = *(const f32x4*)(score + r * (pl.len_pad + kMaxTree) + at);
 #pragma unroll
     for (int r = 0; r < kStoredRows; ++r)
-      if (r < n_rows && vote[r] != 0.f && lse2[r] != neg_inf())
+      if (r < n_rows && coef[r] != 0.f)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          acc[i] += vote[r] * exp2_(x[r][i] - lse2[r]);
+          acc[i] += coef[r] * t.exp_of(x[r][i] - row_m[r]);
     return acc;
   };
-  const int64_t key = ((int64_t)kb * kThreads + tid) * 4;
   if (key < tr.len) {
     const f32x4 m = sum(key);
     float* w = c.weight + (int64_t)unit * c.cap + key;
@@ -779,14 +821,9 @@ __global__ __launch_bounds__(kThreads) void mass_stored_kernel(
     }
   }
   if (kb == 0 && t.w_new && 4 * tid < tr.n) {
-    if (!t.k_new) {
-      for (int i = 0; i < 4 && 4 * tid + i < tr.n; ++i)
-        t.w_new[(int64_t)(tr.first + 4 * tid + i) * c.hkv + kvh] = 0.f;
-    } else {
-      const f32x4 m = sum(pl.len_pad + 4 * tid);
-      for (int i = 0; i < 4 && 4 * tid + i < tr.n; ++i)
-        t.w_new[(int64_t)(tr.first + 4 * tid + i) * c.hkv + kvh] = m[i];
-    }
+    const f32x4 m = t.k_new ? sum(pl.len_pad + 4 * tid) : f32x4{};
+    for (int i = 0; i < 4 && 4 * tid + i < tr.n; ++i)
+      t.w_new[(int64_t)(tr.first + 4 * tid + i) * c.hkv + kvh] = m[i];
   }
 }
 
@@ -806,7 +843,7 @@ __global__ __launch_bounds__(kThreads) void mass_kernel(const CacheView c,
   const Tree tr = tree_of(c, t, seq);
   if (tr.n == 0) return;
   const int group = t.hq / c.hkv, n_rows = tr.n * group;
-  const Parts pt = parts_of(tr, t.k_new != nullptr, P::KT, pl.splits);
+  constexpr int kWaves = kThreads / 64;
   const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int cached = (tr.len + TK - 1) / TK;
@@ -843,16 +880,16 @@ __global__ __launch_bounds__(kThreads) void mass_kernel(const CacheView c,
     }
   }
   const int padded = pl.row_blocks * 16 * pl.row_tiles;
-  const int64_t base = (int64_t)unit * pl.splits * padded;
   f32x4 acc[NK] = {};
   for (int r0 = 0; r0 < n_rows; r0 += 16) {
     const int r = min(r0 + c16, n_rows - 1), tok = r / group;
     typename P::Row q;
     P::load_row(q, t.q + ((int64_t)(tr.first + tok) * t.hq + kvh * group +
                           r % group) * (D * P::ES) + 16 * g);
-    const float lse2 = row_lse2(t, base + r, padded, pt.used);
-    float vote = t.vote ? t.vote[tr.first + tok] : 1.f;
-    if (r0 + c16 >= n_rows || lse2 == neg_inf()) vote = 0.f;
+    const float m = t.row_m[(int64_t)unit * padded + r];
+    float coef = t.row_inv[(int64_t)unit * padded + r];
+    const float vote = t.vote ? t.vote[tr.first + tok] : 1.f;
+    coef = vote == 0.f || r0 + c16 >= n_rows ? 0.f : coef * vote;
     const uint64_t sees = draft ? __shfl(anc, tok) >> j0 : 0;
 #pragma unroll
     for (int h = 0; h < NK; ++h) {
@@ -860,8 +897,8 @@ __global__ __launch_bounds__(kThreads) void mass_kernel(const CacheView c,
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const bool see = !draft || (sees >> (16 * h + 4 * g + i) & 1);
-        if (vote != 0.f && see && 4 * g + i < n[h])
-          acc[h][i] += vote * exp2_(x[i] * t.scale_log2 - lse2);
+        if (coef != 0.f && see && 4 * g + i < n[h])
+          acc[h][i] += coef * t.exp_of(x[i] - m);
       }
     }
   }
@@ -888,21 +925,19 @@ hipError_t launch_tree(const CacheView& c, const TreePlan& pl,
   const int64_t blocks = (units + 7) / 8 * 8 * pl.row_blocks;
   if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
   const dim3 grid((unsigned)blocks), block(kThreads);
+  const dim3 waves(64 * waves_of(pl.row_tiles));
   if (pl.stored)
-    tree_kernel<P, D, 1, true><<<grid, block, 0, s>>>(c, pl, t);
+    tree_kernel<P, D, 1, true><<<grid, waves, 0, s>>>(c, pl, t);
   else if (pl.row_tiles == 1)
-    tree_kernel<P, D, 1, false><<<grid, block, 0, s>>>(c, pl, t);
+    tree_kernel<P, D, 1, false><<<grid, waves, 0, s>>>(c, pl, t);
   else if (pl.row_tiles == 2)
-    tree_kernel<P, D, 2, false><<<grid, block, 0, s>>>(c, pl, t);
+    tree_kernel<P, D, 2, false><<<grid, waves, 0, s>>>(c, pl, t);
   else if constexpr (P::ES == 2)
-    tree_kernel<P, D, 4, false><<<grid, block, 0, s>>>(c, pl, t);
+    tree_kernel<P, D, 4, false><<<grid, waves, 0, s>>>(c, pl, t);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  int64_t join = 0;
-  if (pl.splits > 1) {
-    constexpr int kRows = kThreads / (D / 4);
-    join = ((int64_t)c.n_seq * c.hkv * pl.rows + kRows - 1) / kRows;
-  }
+  const int64_t join =
+      pl.splits > 1 ? (int64_t)c.n_seq * c.hkv * pl.rows : 0;
   if (pl.stored) {
     const int kb = std::max(1, (t.max_len + 4 * kThreads - 1) / (4 * kThreads));
     const int64_t n = join + (int64_t)c.n_seq * c.hkv * kb;
@@ -920,7 +955,7 @@ hipError_t launch_tree(const CacheView& c, const TreePlan& pl,
   if (t.accumulate) {
     constexpr int TK = 16 * kMassHalves<P>;
     const int tiles = (t.max_len + TK - 1) / TK + (t.max_tree + TK - 1) / TK;
-    const int kb = (tiles + kWaves - 1) / kWaves;
+    const int kb = (tiles + kThreads / 64 - 1) / (kThreads / 64);
     const int64_t n = (int64_t)c.n_seq * c.hkv * kb;
     if (n > 0x7FFFFFFF) return hipErrorInvalidValue;
     mass_kernel<P, D><<<dim3((unsigned)n), block, 0, s>>>(c, pl, t, kb);
@@ -940,10 +975,14 @@ TreePlan plan_tree(const CacheView& c, int32_t hq, int32_t max_tree,
   p.row_blocks = (p.rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles);
   const int64_t tiles =
       ((int64_t)max_len + kt - 1) / kt + (max_tree + kt - 1) / kt;
-  // about 2,048 work-groups for the 256 CUs, each with kMinTiles at least
+  // A sequence whose tiles its work-group passes in eight rounds is not split:
+  // that takes less than the second launch. Otherwise about 1,024 work-groups
+  // for the 256 CUs, two rounds a work-group at least.
+  const int w = waves_of(p.row_tiles);
   const int64_t units = (int64_t)c.n_seq * c.hkv * p.row_blocks;
-  int64_t splits = std::max<int64_t>(1, 2048 / units);
-  splits = std::min(splits, (tiles + kMinTiles - 1) / kMinTiles);
+  int64_t splits = std::min<int64_t>(kMaxSplits, std::max<int64_t>(1, 1024 / units));
+  splits = std::min(splits, (tiles + 2 * w - 1) / (2 * w));
+  if (tiles <= 8 * w) splits = 1;
   p.splits = (int32_t)std::max<int64_t>(1, splits);
   p.stored = accumulate && p.rows <= kStoredRows;
   p.len_pad = ((int64_t)max_len + 31) / 32 * 32;
@@ -956,8 +995,10 @@ TreePlan plan_tree(const CacheView& c, int32_t hq, int32_t max_tree,
   const size_t part = (size_t)c.n_seq * c.hkv * p.splits * p.row_blocks * 16 *
                       p.row_tiles;
   p.pO = take(p.splits > 1 ? part * c.d * 4 : 0);
-  p.pM = take(p.splits > 1 || accumulate ? part * 4 : 0);
-  p.pL = take(p.splits > 1 || accumulate ? part * 4 : 0);
+  p.pM = take(p.splits > 1 ? part * 4 : 0);
+  p.pL = take(p.splits > 1 ? part * 4 : 0);
+  p.row_m = take(accumulate ? part / p.splits * 4 : 0);
+  p.row_inv = take(accumulate ? part / p.splits * 4 : 0);
   p.score = take(p.stored ? (size_t)c.n_seq * c.hkv * p.rows *
                                 (p.len_pad + kMaxTree) * 4
                           : 0);
