@@ -72,17 +72,18 @@ hipError_t launch_cache_evict(const CacheView& c, const EvictCall& e,
 
 // A row's reference moves when a logit passes it by this (log2 units): the
 // probabilities stay below 2^8, and fp32 sums and bf16 probabilities keep
-// their relative precision at any such scale. References and logits are kept
-// as q.k and scaled after their difference is taken, so that the keys that
-// matter, near the reference, carry no rounding of the scaled logit.
+// their relative precision at any such scale.
 constexpr float kTreeSlack = 8.0f;
 
 // How a tree attention call is split (host, from its bounds alone).
 struct TreePlan {
   int32_t rows;        // most query rows of a kv head: group * max_tree
   int32_t row_tiles;   // 16-row tiles that a wave takes (1, 2 or 4)
-  int32_t row_blocks;  // blocks of 16 * row_tiles rows
-  int32_t splits;      // of the keys
+  int32_t wide;        // many rows: the kernel that shares keys through LDS
+  int32_t row_blocks;  // work-groups that the rows take
+  int32_t padded;      // rows, to whole work-groups
+  int32_t splits;      // of the keys, by work-group
+  int32_t parts;       // of the keys at most (wide: two a split)
   int32_t stored;      // accumulate: the scores pass through the workspace
   int64_t len_pad;     // max_len rounded up, of the stored scores
   // workspace offsets and total, bytes
@@ -99,25 +100,25 @@ struct TreeCall {
   float* lse;                // may be null
   const float* vote;         // may be null
   float* w_new;              // may be null
-  float scale, scale_log2;   // of the logits, and times log2(e)
-  float slack;               // how far (in q.k) a logit may pass a reference
+  float scale_log2;          // of the logits, times log2(e)
   float decay;
   int32_t hq, n_tok, max_tree, max_len, accumulate;
-  float* pO;                 // [seq][kv head][split][row][d]
-  float* pM;                 // [seq][kv head][split][row] reference, as q.k
+  float* pO;                 // [seq][kv head][part][row][d]
+  float* pM;                 // [seq][kv head][part][row] reference, log2 units
   float* pL;                 //                            and sum
   float* row_m;              // [seq][kv head][row] the same, over the splits:
   float* row_inv;            // reference and 1 / sum (accumulate)
   float* score;              // [seq][kv head][row][len_pad + 64] q.k
 
-  // exp(scale * x), x the difference of two q.k
-  __device__ __forceinline__ float exp_of(float x) const {
-    return __builtin_amdgcn_exp2f(x * scale_log2);
+  // exp2 of a logit (as q.k) over a reference (log2 units). One rounding, of
+  // a value that is small where it matters; the reference's own cancels.
+  __device__ __forceinline__ float exp_of(float x, float ref) const {
+    return __builtin_amdgcn_exp2f(__builtin_fmaf(x, scale_log2, -ref));
   }
   __device__ __forceinline__ float lse_of(float m, float sum) const {
     return sum == 0.f ? -__builtin_inff()
-                      : m * scale + __builtin_amdgcn_logf(sum) *
-                                        0.69314718055994530942f;
+                      : (m + __builtin_amdgcn_logf(sum)) *
+                            0.69314718055994530942f;
   }
 };
 TreePlan plan_tree(const CacheView& c, int32_t hq, int32_t max_tree,

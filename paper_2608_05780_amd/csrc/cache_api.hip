@@ -190,9 +190,7 @@ evisel_status evisel_tree_attention(
   t.lse = lse;
   t.vote = accumulate ? vote : nullptr;
   t.w_new = accumulate ? w_new : nullptr;
-  t.scale = softmax_scale;
   t.scale_log2 = softmax_scale * 1.4426950408889634f;
-  t.slack = std::min(evisel::kTreeSlack / t.scale_log2, 1e30f);
   t.decay = decay;
   t.hq = hq;
   t.n_tok = n_tok;

@@ -2,25 +2,20 @@
 // and the accumulated attention weight.
 #include <algorithm>
 
+#include "attn_tiles.h"
 #include "cache.h"
 
 namespace evisel {
 namespace {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-typedef float f32x8 __attribute__((ext_vector_type(8)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kThreads = 256;   // of the kernels behind the attention itself
 constexpr int kMaxTree = 64;
 constexpr int kMaxSplits = 128;
 // Wavefronts of a work-group that takes 16 RT rows.
 constexpr int waves_of(int row_tiles) { return row_tiles == 4 ? 4 : 8; }
 
-__device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
 // Over the four lanes that hold one query row (lane % 16).
 __device__ __forceinline__ float row_max(float x) {
   x = fmaxf(x, __shfl_xor(x, 16));
@@ -253,6 +248,25 @@ __device__ __forceinline__ Parts parts_of(const Tree& r, bool drafts, int kt,
   return p;
 }
 
+// Many rows (wide): a work-group takes 256 of them, kWideRows a wavefront,
+// and where half of the wavefronts or fewer have rows, two share them, each
+// with one half of the keys.
+constexpr int kWideRt = 2, kWideRows = 16 * kWideRt;
+constexpr int kWideWaves = 8;
+constexpr int kWideBlock = kWideRows * kWideWaves;
+constexpr int kWideKeys = 64;   // of a stage
+__device__ __forceinline__ int key_halves(int n_rows, int row0) {
+  return n_rows - row0 <= kWideBlock / 2 ? 2 : 1;
+}
+// The parts that row r of a sequence is joined from.
+template <class P>
+__device__ __forceinline__ int row_parts(const TreePlan& pl, const Tree& tr,
+                                         bool drafts, int n_rows, int r) {
+  if (!pl.wide) return parts_of(tr, drafts, P::KT, pl.splits).used;
+  return parts_of(tr, drafts, kWideKeys, pl.splits).used *
+         key_halves(n_rows, r / kWideBlock * kWideBlock);
+}
+
 // Which drafted tokens token `lane` sees: itself and its ancestors. The lanes'
 // parents are followed by doubling, six times for 64 tokens.
 __device__ __forceinline__ uint64_t ancestors(const TreeCall& t, const Tree& r,
@@ -276,24 +290,27 @@ struct Where {
   int64_t off[NH];
   int n[NH];
 };
+// The page of slot `slot` (past the end: the last page, which is not used).
+__device__ __forceinline__ int page_of(const CacheView& c, int seq, int len,
+                                       int slot) {
+  return ((ScalarTable)c.table)[(int64_t)seq * c.max_pages +
+                                (max(min(slot, len - 1), 0) >> c.page_shift)];
+}
+// Rows slot .. slot + 15 of page `id`: their address and their number.
+__device__ __forceinline__ int place(int64_t& off, const CacheView& c, int id,
+                                     int64_t head, int len, int slot) {
+  const bool ok = slot < len && (uint32_t)id < (uint32_t)c.n_pages;
+  off = (ok ? id : 0) * c.page_bytes + head +
+        (ok ? (int64_t)(slot & ((1 << c.page_shift) - 1)) : 0) * c.token_bytes;
+  return ok ? min(16, len - slot) : 0;
+}
 template <int NH>
 __device__ __forceinline__ void find(Where<NH>& w, const CacheView& c, int seq,
                                      int64_t head, int len, int slot0) {
 #pragma unroll
-  for (int h = 0; h < NH; ++h) {
-    const int s = slot0 + 16 * h;
-    w.off[h] = head;
-    w.n[h] = 0;
-    if (s < len) {
-      const int id = ((ScalarTable)c.table)[(int64_t)seq * c.max_pages +
-                                            (s >> c.page_shift)];
-      if (id >= 0 && id < c.n_pages) {
-        w.off[h] = id * c.page_bytes + head +
-                   (int64_t)(s & ((1 << c.page_shift) - 1)) * c.token_bytes;
-        w.n[h] = min(16, len - s);
-      }
-    }
-  }
+  for (int h = 0; h < NH; ++h)
+    w.n[h] = place(w.off[h], c, page_of(c, seq, len, slot0 + 16 * h), head, len,
+                   slot0 + 16 * h);
 }
 
 template <class P>
@@ -320,7 +337,7 @@ template <class P, int D, int RT>
 struct Rows {
   typename P::Row q[RT];
   f32x4 o[RT][P::NT];
-  float m[RT], l[RT];   // reference (q.k) and sum
+  float m[RT], l[RT];   // reference (log2 units) and sum
 
   __device__ __forceinline__ void logits(f32x4 (&x)[RT][P::NH],
                                          const typename P::Row (&k)[P::NH]) {
@@ -340,33 +357,51 @@ struct Rows {
         for (int i = 0; i < 4; ++i)
           if (!(vis[rt] >> (4 * h + i) & 1)) x[rt][h][i] = neg_inf();
   }
-  // Logits to probabilities (against the rows' references) and their sums.
-  __device__ __forceinline__ void softmax(f32x4 (&x)[RT][P::NH],
-                                          const TreeCall& t) {
+  // Moves the references of rows that a logit has passed.
+  __device__ __forceinline__ void refer(const f32x4 (&x)[RT][P::NH],
+                                        const TreeCall& t) {
+    float top[RT];
+    bool past = false;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      float top = neg_inf();
+      top[rt] = neg_inf();
 #pragma unroll
       for (int h = 0; h < P::NH; ++h)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) top = fmaxf(top, x[rt][h][i]);
-      if (__any(top > m[rt] + t.slack)) {
-        const float next = fmaxf(m[rt], row_max(top));
-        const float a = m[rt] == neg_inf() ? 0.f : t.exp_of(m[rt] - next);
+        for (int i = 0; i < 4; ++i) top[rt] = fmaxf(top[rt], x[rt][h][i]);
+      past = past || top[rt] * t.scale_log2 > m[rt] + kTreeSlack;
+    }
+    if (__any(past)) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        const float next = fmaxf(m[rt], row_max(top[rt]) * t.scale_log2);
+        const float a = m[rt] == neg_inf() ? 0.f : exp2_(m[rt] - next);
         m[rt] = next;
         l[rt] *= a;
 #pragma unroll
         for (int u = 0; u < P::NT; ++u) o[rt][u] *= a;
       }
+    }
+  }
+  // Logits to probabilities against the references, and their sums.
+  __device__ __forceinline__ void weigh(f32x4 (&x)[RT][P::NH],
+                                        const TreeCall& t) {
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
       const float ref = m[rt] == neg_inf() ? 0.f : m[rt];
 #pragma unroll
       for (int h = 0; h < P::NH; ++h)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          x[rt][h][i] = t.exp_of(x[rt][h][i] - ref);
+          x[rt][h][i] = t.exp_of(x[rt][h][i], ref);
           l[rt] += x[rt][h][i];
         }
     }
+  }
+  __device__ __forceinline__ void softmax(f32x4 (&x)[RT][P::NH],
+                                          const TreeCall& t) {
+    refer(x, t);
+    weigh(x, t);
   }
   __device__ __forceinline__ void add(const typename P::ValT& v,
                                       const f32x4 (&x)[RT][P::NH]) {
@@ -374,6 +409,101 @@ struct Rows {
     for (int rt = 0; rt < RT; ++rt) P::pv(o[rt], v, x[rt]);
   }
 };
+
+// A tile of drafted tokens j0 .. j0 + KT - 1: every row sees keys of its own.
+// score: where a row's logits of the cache start, or null; probs: 16 RT KT
+// floats of LDS of the wavefront's own.
+template <class P, int D, int RT>
+__device__ __forceinline__ void take_drafts(Rows<P, D, RT>& rows,
+                                            const CacheView& c,
+                                            const TreeCall& t, const Tree& tr,
+                                            int kvh, int row0, int n_rows,
+                                            int j0, float* score,
+                                            int64_t len_pad, float* probs) {
+  constexpr int KT = P::KT, NH = P::NH;
+  const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4;
+  const int group = t.hq / c.hkv;
+  const uint64_t anc = ancestors(t, tr, lane);
+  const int64_t step = (int64_t)c.hkv * (D * P::ES);
+  const int64_t base = (int64_t)tr.first * step + kvh * (D * P::ES);
+  struct {
+    typename P::Row k[NH];
+    typename P::Val v;
+  } x;
+  bool fine = true;
+#pragma unroll
+  for (int h = 0; h < NH; ++h) {
+    const int j = min(j0 + 16 * h + c16, tr.n - 1);
+    P::load_row(x.k[h], t.k_new + base + j * step + 16 * g);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int jv = j0 + 16 * h + 4 * g + i;
+      if (jv < tr.n) {
+        P::load_val(x.v.x[h][i], t.v_new + base + jv * step + c16 * P::kLaneV);
+        fine = fine && P::finite(x.v.x[h][i]);
+      } else {
+        P::zero_val(x.v.x[h][i]);
+      }
+    }
+  }
+  uint32_t vis[RT];
+  uint32_t sees[RT];   // by key of the tile
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int r = row0 + 16 * rt + c16;
+    const uint64_t all = __shfl(anc, min(r, n_rows - 1) / group);
+    sees[rt] = r < n_rows ? (uint32_t)(all >> j0) : 0u;
+    vis[rt] = 0;
+#pragma unroll
+    for (int h = 0; h < NH; ++h)
+      vis[rt] |= (sees[rt] >> (16 * h + 4 * g) & 15u) << (4 * h);
+  }
+  f32x4 p[RT][NH];
+  rows.logits(p, x.k);
+  rows.hide(p, vis);
+  if (score)
+#pragma unroll
+    for (int h = 0; h < NH; ++h)
+      *(f32x4*)(score + len_pad + j0 + 16 * h) = p[0][h];
+  rows.softmax(p, t);
+  // A value that is not finite reaches the rows that see its token and no
+  // other: it is left out of the product, whose zeros it would spoil, and
+  // added by itself.
+  const bool plain = __all(fine);
+  if (!plain) {
+#pragma unroll
+    for (int h = 0; h < NH; ++h)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) P::drop_infinite(x.v.x[h][i]);
+  }
+  typename P::ValT vt;
+  P::turn(vt, x.v);
+  rows.add(vt, p);
+  if (plain) return;
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+    for (int h = 0; h < NH; ++h)
+      *(f32x4*)(probs + (16 * rt + c16) * KT + 16 * h + 4 * g) = p[rt][h];
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  for (int j = 0; j < KT && j0 + j < tr.n; ++j) {
+    const char* v = t.v_new + base + (j0 + j) * step;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      if (!(sees[rt] >> j & 1)) continue;
+      const float pj = probs[(16 * rt + c16) * KT + j];
+#pragma unroll
+      for (int u = 0; u < P::NT; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float e = P::element(v, P::col(g, i, u));
+          if (!__builtin_isfinite(e)) rows.o[rt][u][i] += pj * e;
+        }
+    }
+  }
+  __builtin_amdgcn_wave_barrier();
+}
 
 // One work-group: a sequence, a kv head, a run of its key tiles (a split) and
 // 16 RT of its query rows. The wavefronts take the run's tiles in turn, each
@@ -487,89 +617,9 @@ __global__ __launch_bounds__(64 * waves_of(RT), RT == 4 ? 1 : 2) void tree_kerne
   }
   for (tile = t0 + wave; tile < t1; tile += kWaves) {
     if (tile < pt.cached) continue;
-    // drafted tokens: every row has keys of its own
-    const int j0 = (tile - pt.cached) * KT;
-    const uint64_t anc = ancestors(t, tr, lane);
-    const int64_t step = (int64_t)c.hkv * (D * P::ES);
-    const int64_t base = (int64_t)tr.first * step + kvh * (D * P::ES);
-    struct {
-      typename P::Row k[NH];
-      typename P::Val v;
-    } x;
-    bool fine = true;
-#pragma unroll
-    for (int h = 0; h < NH; ++h) {
-      const int j = min(j0 + 16 * h + c16, tr.n - 1);
-      P::load_row(x.k[h], t.k_new + base + j * step + 16 * g);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int jv = j0 + 16 * h + 4 * g + i;
-        if (jv < tr.n) {
-          P::load_val(x.v.x[h][i], t.v_new + base + jv * step + c16 * P::kLaneV);
-          fine = fine && P::finite(x.v.x[h][i]);
-        } else {
-          P::zero_val(x.v.x[h][i]);
-        }
-      }
-    }
-    uint32_t vis[RT];
-    uint32_t sees[RT];   // by key of the tile
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      const int r = row0 + 16 * rt + c16;
-      const uint64_t all = __shfl(anc, min(r, n_rows - 1) / group);
-      sees[rt] = r < n_rows ? (uint32_t)(all >> j0) : 0u;
-      vis[rt] = 0;
-#pragma unroll
-      for (int h = 0; h < NH; ++h)
-        vis[rt] |= (sees[rt] >> (16 * h + 4 * g) & 15u) << (4 * h);
-    }
-    f32x4 p[RT][NH];
-    rows.logits(p, x.k);
-    rows.hide(p, vis);
-    if (SCORE && score[0])
-#pragma unroll
-      for (int h = 0; h < NH; ++h)
-        *(f32x4*)(score[0] + pl.len_pad + j0 + 16 * h) = p[0][h];
-    rows.softmax(p, t);
-    // A value that is not finite reaches the rows that see its token and no
-    // other: it is left out of the product, whose zeros it would spoil, and
-    // added by itself.
-    const bool plain = __all(fine);
-    if (!plain) {
-#pragma unroll
-      for (int h = 0; h < NH; ++h)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) P::drop_infinite(x.v.x[h][i]);
-    }
-    typename P::ValT vt;
-    P::turn(vt, x.v);
-    rows.add(vt, p);
-    if (plain) continue;
-    float* probs = so[wave];
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-      for (int h = 0; h < NH; ++h)
-        *(f32x4*)(probs + (16 * rt + c16) * KT + 16 * h + 4 * g) = p[rt][h];
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    for (int j = 0; j < KT && j0 + j < tr.n; ++j) {
-      const char* v = t.v_new + base + (j0 + j) * step;
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        if (!(sees[rt] >> j & 1)) continue;
-        const float pj = probs[(16 * rt + c16) * KT + j];
-#pragma unroll
-        for (int u = 0; u < P::NT; ++u)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float e = P::element(v, P::col(g, i, u));
-            if (!__builtin_isfinite(e)) rows.o[rt][u][i] += pj * e;
-          }
-      }
-    }
-    __builtin_amdgcn_wave_barrier();
+    take_drafts<P, D, RT>(rows, c, t, tr, kvh, row0, n_rows,
+                          (tile - pt.cached) * KT,
+                          SCORE ? score[0] : nullptr, pl.len_pad, so[wave]);
   }
 
   // the wavefronts' rows
@@ -584,15 +634,15 @@ __global__ __launch_bounds__(64 * waves_of(RT), RT == 4 ? 1 : 2) void tree_kerne
   __syncthreads();
   constexpr int kCols = 16 * D / (64 * kWaves);   // of a thread
   const int er = threadIdx.x / (D / kCols), ec = threadIdx.x % (D / kCols);
-  const int padded = pl.row_blocks * 16 * RT;
-  const int64_t part = ((int64_t)unit * pl.splits + split) * padded;
+  const int padded = pl.padded;
+  const int64_t part = ((int64_t)unit * pl.parts + split) * padded;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     float top = neg_inf();
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sm[w][16 * rt + c16]);
     const float f =
-        rows.m[rt] == neg_inf() ? 0.f : t.exp_of(rows.m[rt] - top);
+        rows.m[rt] == neg_inf() ? 0.f : exp2_(rows.m[rt] - top);
 #pragma unroll
     for (int u = 0; u < P::NT; ++u)
 #pragma unroll
@@ -608,7 +658,7 @@ __global__ __launch_bounds__(64 * waves_of(RT), RT == 4 ? 1 : 2) void tree_kerne
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
         const float mw = sm[w][16 * rt + er];
-        sum += (mw == neg_inf() ? 0.f : t.exp_of(mw - big)) *
+        sum += (mw == neg_inf() ? 0.f : exp2_(mw - big)) *
                sl[w][16 * rt + er];
       }
       float x[kCols] = {};
@@ -647,6 +697,372 @@ __global__ __launch_bounds__(64 * waves_of(RT), RT == 4 ? 1 : 2) void tree_kerne
   }
 }
 
+// Many query rows of bf16: here the matrix cores are the bound, and the
+// wavefronts, 32 rows each, share every key. A stage of 64 keys passes from
+// memory straight into one of three LDS buffers, two stages ahead of the one
+// that is worked on; one barrier a stage.
+// The products are those of tree_kernel, but V's operand comes from LDS by
+// transposing reads: four lanes a key name the 16 columns, and lane c holds
+// column c of four keys; the columns are chosen so that a lane's share of O is
+// one run. Both buffers are swizzled in 16-byte chunks so that the lanes of
+// one read touch every bank once.
+template <class P, int D>
+__global__ __launch_bounds__(64 * kWideWaves, kWideRt == 2 ? 2 : 1) void tree_wide_kernel(
+    const CacheView c, const TreePlan pl, const TreeCall t) {
+  constexpr int RT = kWideRt, KT = P::KT, NH = P::NH, NT = P::NT;
+  constexpr int RC = D * P::ES / 16;             // 16-byte chunks of a row
+  constexpr int kRuns = kWideKeys / 16;          // runs of 16 keys: one page
+  constexpr int kBytes = kWideKeys * D * P::ES;
+  __shared__ __attribute__((aligned(16))) char buf[3][2][kBytes];   // K, V
+  __shared__ __attribute__((aligned(16))) float probs[kWideWaves][16 * RT * KT];
+  __shared__ int odd;   // a drafted value that is not finite
+  const int xcd = blockIdx.x % 8, y = blockIdx.x / 8;
+  const int rb = y % pl.row_blocks;
+  int unit = y / pl.row_blocks * 8 + xcd;
+  if (unit >= c.n_seq * c.hkv * pl.splits) return;
+  const int split = unit % pl.splits;
+  unit /= pl.splits;
+  const int kvh = unit % c.hkv, seq = unit / c.hkv;
+  const Tree tr = tree_of(c, t, seq);
+  const int group = t.hq / c.hkv, n_rows = tr.n * group;
+  const int block0 = rb * kWideBlock;
+  if (block0 >= n_rows) return;
+  const Parts pt =
+      parts_of(tr, t.k_new != nullptr, kWideKeys, pl.splits);
+  if (split >= pt.used) return;
+  const int tid = threadIdx.x, lane = tid & 63, c16 = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int halves = key_halves(n_rows, block0);
+  // the steps of a stage that this wavefront takes: from `half` on, every
+  // halves-th
+  const int half = halves == 2 ? wave / (kWideWaves / 2) : 0;
+  const int row0 =
+      block0 + (halves == 2 ? wave % (kWideWaves / 2) : wave) * kWideRows;
+  const bool works = row0 < n_rows;
+  const int64_t head = kvh * c.head_bytes;
+
+  Rows<P, D, RT> rows;
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int r = row0 + 16 * rt + c16;
+    rows.m[rt] = neg_inf();
+    rows.l[rt] = 0.f;
+#pragma unroll
+    for (int i = 0; i < NT; ++i) rows.o[rt][i] = f32x4{};
+    if (r < n_rows) {
+      const int tok = r / group, qh = r % group;
+      P::load_row(rows.q[rt],
+                  t.q + ((int64_t)(tr.first + tok) * t.hq + kvh * group + qh) *
+                            (D * P::ES) + 16 * g);
+    } else {
+      P::zero_row(rows.q[rt]);
+    }
+  }
+
+  const int s0 = split * pt.per, s1 = min(s0 + pt.per, pt.cached);
+  auto k_swizzle = [](int r) { return RC == 16 ? r & 15 : (r >> 1) & 7; };
+  // a transposing read names four keys, and of each four chunks, every
+  // fourth (D = 64: every second, of two keys in a line of 256 bytes)
+  auto v_swizzle = [](int r) { return RC == 16 ? r & 3 : (r >> 1) & 1; };
+  // A wavefront sends for K or V of one run of 16 keys, which is in one page:
+  // 1 KB a load, its rows neighbours in LDS; the swizzle is in what a lane
+  // fetches. The page is looked up a stage before.
+  constexpr int kLoads = 16 * RC / 64;      // of a run
+  constexpr int kLoadRows = 64 / RC;        // of a load
+  static_assert(kWideWaves == 2 * kRuns, "one run of K or V a wavefront");
+  const int my_run = wave / 2;
+  const char* const pool = wave % 2 ? c.v : c.k;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(EV_LDS char*)&buf[0][0][0] +
+                        (uint32_t)(wave % 2 * kBytes + my_run * 256 * RC);
+  uint32_t from[kLoads];
+#pragma unroll
+  for (int j = 0; j < kLoads; ++j) {
+    const int r = j * kLoadRows + lane / RC;
+    const int ch = lane % RC ^ (wave % 2 ? v_swizzle(r) : k_swizzle(r));
+    from[j] = (uint32_t)r * c.token_bytes + 16 * ch;
+  }
+  int page = 0;
+  auto look = [&](int stage) {
+    page = page_of(c, seq, tr.len, stage * kWideKeys + 16 * my_run);
+  };
+  auto fetch = [&](int stage, int b) {
+    int64_t at;
+    place(at, c, page, head, tr.len, stage * kWideKeys + 16 * my_run);
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j)
+      lds_dma16(lds0 + (uint32_t)(2 * b * kBytes + j * 1024), pool + at,
+                from[j]);
+    look(stage + 1);
+  };
+  // Keys that are there of run i of a stage, where not all need be.
+  auto there = [&](int stage, int i) {
+    const int slot = stage * kWideKeys + 16 * i;
+    int64_t at;
+    return place(at, c, page_of(c, seq, tr.len, slot), head, tr.len, slot);
+  };
+  // Whether a page of this split is missing: then every stage is looked
+  // through, otherwise only one that passes the end.
+  int missing = 0;
+  for (int i = s0 * kRuns + tid; i < s1 * kRuns; i += 64 * kWideWaves)
+    missing |= 16 * i < tr.len &&
+               (uint32_t)c.table[(int64_t)seq * c.max_pages +
+                                 (16 * i >> c.page_shift)] >=
+                   (uint32_t)c.n_pages;
+  const bool holes = __syncthreads_or(missing);
+  auto partial = [&](int stage) {
+    return holes || (stage + 1) * kWideKeys > tr.len;
+  };
+  // Waits for a stage, not for the `later` one sent for after it. Keys past
+  // the end or without a page: no row sees them, and their values must not
+  // meet a probability of zero.
+  auto arrive = [&](int stage, int b, bool later) {
+    if (later)
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
+    else
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (!partial(stage)) return;
+    for (int u = tid; u < kWideKeys * RC; u += 64 * kWideWaves)
+      if (u / RC % 16 >= there(stage, u / RC / 16))
+        *(u32x4*)&buf[b][1][u * 16] = u32x4{};
+    __syncthreads();
+  };
+  typename P::Row k[NH];
+  auto read_k = [&](int b, int sub) {
+#pragma unroll
+    for (int h = 0; h < NH; ++h) {
+      const int r = KT * sub + 16 * h + c16;
+#pragma unroll
+      for (int j = 0; j < P::KS; ++j)
+        k[h].x[j] = *(const bf16x8*)&buf[b][0][(r * RC + ((g + 4 * j) ^
+                                                          k_swizzle(r))) * 16];
+    }
+  };
+  // V's operands of a step: tile u's column of lane c is D / 4 (c / 4) + 4u +
+  // c % 4; lane j of 16 names the row 4g + j / 4 and the columns of j % 4
+  auto read_v = [&](bf16x8 (&va)[NT], int b, int sub) {
+    const int r = 4 * g + (c16 >> 2);   // and 16 below it
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+      const int col = D / 4 * (c16 & 3) + 4 * u;
+      const int at = ((KT * sub + r) * RC + ((col / 8) ^ v_swizzle(r))) * 16 +
+                     (col % 8) * 2;
+      const EV_LDS char* p = (const EV_LDS char*)buf[b][1] + at;
+      const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (EV_LDS i16x4*)p);
+      const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (EV_LDS i16x4*)(p + 16 * RC * 16));
+      const i16x4 both[2] = {lo, hi};
+      va[u] = __builtin_bit_cast(bf16x8, both);
+    }
+  };
+  auto add_v = [&](const bf16x8 (&va)[NT], const f32x4 (&x)[RT][NH]) {
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const f32x8 pf = __builtin_shufflevector(x[rt][0], x[rt][1], 0, 1, 2, 3,
+                                               4, 5, 6, 7);
+      const bf16x8 pb = __builtin_convertvector(pf, bf16x8);
+#pragma unroll
+      for (int u = 0; u < NT; ++u)
+        rows.o[rt][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+            va[u], pb, rows.o[rt][u], 0, 0, 0);
+    }
+  };
+  // The probabilities of the step before, and V's product with them, wait for
+  // this step's logits: nothing then stands between the two products, and the
+  // exponentials run beside the matrix cores. x: the logits of the step
+  // before; va: its values.
+  f32x4 x[RT][NH];
+  bf16x8 va[NT];
+#pragma unroll
+  for (int u = 0; u < NT; ++u) va[u] = bf16x8{};
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+    for (int h = 0; h < NH; ++h)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[rt][h][i] = neg_inf();
+  // 32 keys of a stage, whose K is in k; `next`: the step to read K of then
+  auto step = [&](int stage, int b, int sub, int next) {
+    f32x4 y[RT][NH];
+    // (ahead of the other wavefront of its SIMD, which is at its softmax then)
+    __builtin_amdgcn_s_setprio(2);
+    rows.logits(y, k);
+    rows.weigh(x, t);
+    add_v(va, x);
+    __builtin_amdgcn_s_setprio(0);
+    read_v(va, b, sub);
+    read_k(b, next);
+    if (partial(stage)) {
+      uint32_t vis[RT] = {};
+#pragma unroll
+      for (int h = 0; h < NH; ++h) {
+        const int n = there(stage, NH * sub + h);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (4 * g + i < n) vis[0] |= 1u << (4 * h + i);
+      }
+#pragma unroll
+      for (int rt = 1; rt < RT; ++rt) vis[rt] = vis[0];
+      rows.hide(y, vis);
+    }
+    rows.refer(y, t);
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+      for (int h = 0; h < NH; ++h) x[rt][h] = y[rt][h];
+  };
+  static_assert(kWideKeys == 2 * KT, "two steps a stage");
+  // The query rows are in registers before the first stage is sent for: the
+  // compiler does not count those loads, and a wait of its own inside the loop
+  // would be one for the next stage.
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+    for (int j = 0; j < P::KS; ++j) asm volatile("" : "+v"(rows.q[rt].x[j]));
+  if (s0 < s1) {
+    look(s0);
+    fetch(s0, 0);
+    if (s0 + 1 < s1) fetch(s0 + 1, 1);
+    arrive(s0, 0, s0 + 1 < s1);
+    for (int s = s0, b = 0; s < s1; ++s) {
+      const int b1 = b == 2 ? 0 : b + 1, b2 = b1 == 2 ? 0 : b1 + 1;
+      if (s + 2 < s1) fetch(s + 2, b2);
+      if (works) {
+        read_k(b, half);
+        for (int sub = half; sub < 2; sub += halves) step(s, b, sub, sub | 1);
+      }
+      if (s + 1 < s1) arrive(s + 1, b1, s + 2 < s1);
+      b = b1;
+    }
+  }
+  rows.weigh(x, t);
+  add_v(va, x);
+  if (t.k_new && split == pt.used - 1) {
+    // the drafted tokens, one stage; every row has keys of its own
+    const int64_t token = (int64_t)c.hkv * (D * P::ES);
+    const int64_t base = (int64_t)tr.first * token + kvh * (D * P::ES);
+    __syncthreads();   // the buffers are free
+    if (tid == 0) odd = 0;
+    __syncthreads();
+    for (int u = tid; u < kWideKeys * RC; u += 64 * kWideWaves) {
+      const int r = u / RC, ch = u % RC;
+      const int64_t off = base + min(r, tr.n - 1) * token + 16 * ch;
+      *(u32x4*)&buf[0][0][(r * RC + (ch ^ k_swizzle(r))) * 16] =
+          *(const u32x4*)(t.k_new + off);
+      u32x4 v = *(const u32x4*)(t.v_new + off);
+      // A value that is not finite reaches the rows that see its token and no
+      // other: it is left out of the product, whose zeros it would spoil, and
+      // added by itself.
+      bool fine = true;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        if ((v[w] & 0x7F80u) == 0x7F80u) {
+          v[w] &= 0xFFFF0000u;
+          fine = false;
+        }
+        if ((v[w] & 0x7F800000u) == 0x7F800000u) {
+          v[w] &= 0xFFFFu;
+          fine = false;
+        }
+      }
+      if (r >= tr.n) v = u32x4{};
+      if (!fine && r < tr.n) odd = 1;
+      *(u32x4*)&buf[0][1][(r * RC + (ch ^ v_swizzle(r))) * 16] = v;
+    }
+    __syncthreads();
+    const bool plain = __builtin_amdgcn_readfirstlane(odd) == 0;
+    if (works) {
+      const uint64_t anc = ancestors(t, tr, lane);
+      for (int sub = half; sub < 2 && KT * sub < tr.n; sub += halves) {
+        uint32_t vis[RT], sees[RT];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+          const int r = row0 + 16 * rt + c16;
+          const uint64_t all = __shfl(anc, min(r, n_rows - 1) / group);
+          sees[rt] = r < n_rows ? (uint32_t)(all >> (KT * sub)) : 0u;
+          vis[rt] = 0;
+#pragma unroll
+          for (int h = 0; h < NH; ++h)
+            vis[rt] |= (sees[rt] >> (16 * h + 4 * g) & 15u) << (4 * h);
+        }
+        read_k(0, sub);
+        rows.logits(x, k);
+        rows.hide(x, vis);
+        rows.softmax(x, t);
+        read_v(va, 0, sub);
+        add_v(va, x);
+        if (plain) continue;
+        float* pr = probs[wave];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+          for (int h = 0; h < NH; ++h)
+            *(f32x4*)(pr + (16 * rt + c16) * KT + 16 * h + 4 * g) = x[rt][h];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        for (int j = 0; j < KT && KT * sub + j < tr.n; ++j) {
+          const char* v = t.v_new + base + (KT * sub + j) * token;
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) {
+            if (!(sees[rt] >> j & 1)) continue;
+            const float pj = pr[(16 * rt + c16) * KT + j];
+#pragma unroll
+            for (int u = 0; u < NT; ++u)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const float e = P::element(v, D / 4 * g + 4 * u + i);
+                if (!__builtin_isfinite(e)) rows.o[rt][u][i] += pj * e;
+              }
+          }
+        }
+        __builtin_amdgcn_wave_barrier();
+      }
+    }
+  }
+  if (!works) return;
+
+  // every wavefront has its rows to itself: out, or its part of them
+  const int used = pt.used * halves;
+  const int64_t part =
+      ((int64_t)unit * pl.parts + split * halves + half) * pl.padded;
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const float sum = row_sum(rows.l[rt]), big = rows.m[rt];
+    const int r = row0 + 16 * rt + c16;
+    if (r >= n_rows) continue;
+    if (used > 1) {
+      float* dst = t.pO + (part + r) * D + D / 4 * g;
+#pragma unroll
+      for (int u = 0; u < NT; ++u) *(f32x4*)(dst + 4 * u) = rows.o[rt][u];
+      if (g == 0) {
+        t.pM[part + r] = big;
+        t.pL[part + r] = sum;
+      }
+      continue;
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const int tok = r / group, h = kvh * group + r % group;
+    char* dst = t.out + (((int64_t)(tr.first + tok) * t.hq + h) * D +
+                         D / 4 * g) * P::ES;
+#pragma unroll
+    for (int u = 0; u < NT; u += 2) {
+      const f32x8 y8 = __builtin_shufflevector(rows.o[rt][u] * inv,
+                                               rows.o[rt][u + 1] * inv, 0, 1, 2,
+                                               3, 4, 5, 6, 7);
+      *(bf16x8*)(dst + 4 * u * P::ES) = __builtin_convertvector(y8, bf16x8);
+    }
+    if (g == 0) {
+      if (t.lse)
+        t.lse[(int64_t)h * t.n_tok + tr.first + tok] = t.lse_of(big, sum);
+      if (t.accumulate) {
+        t.row_m[(int64_t)unit * pl.padded + r] = big;
+        t.row_inv[(int64_t)unit * pl.padded + r] = inv;
+      }
+    }
+  }
+}
+
 // The join of row r over its sequence's splits, by a work-group: D / 4
 // threads a split, the splits in turn over the groups of D / 4 threads.
 template <class P, int D>
@@ -656,21 +1072,23 @@ __device__ __forceinline__ void join_row(const CacheView& c,
   constexpr int kLanes = D / 4, kGroups = kThreads / kLanes;
   __shared__ __attribute__((aligned(16))) float part[kGroups][D];
   __shared__ float part_l[kGroups];
-  const int padded = pl.row_blocks * 16 * pl.row_tiles;
+  const int padded = pl.padded;
   const int unit = (int)(row / pl.rows), r = (int)(row % pl.rows);
   const int kvh = unit % c.hkv, seq = unit / c.hkv;
   const Tree tr = tree_of(c, t, seq);
   const int group = t.hq / c.hkv;
-  const Parts pt = parts_of(tr, t.k_new != nullptr, P::KT, pl.splits);
-  if (r >= tr.n * group || pt.used == 1) return;
-  const int64_t base = (int64_t)unit * pl.splits * padded + r;
+  if (r >= tr.n * group) return;
+  const int used =
+      row_parts<P>(pl, tr, t.k_new != nullptr, tr.n * group, r);
+  if (used == 1) return;
+  const int64_t base = (int64_t)unit * pl.parts * padded + r;
   const int lane = threadIdx.x & 63;
   // every wavefront finds the largest reference for itself
   float big = neg_inf();
   static_assert(kMaxSplits <= 128, "two a lane");
 #pragma unroll
   for (int u = 0; u < kMaxSplits / 64; ++u)
-    if (lane + 64 * u < pt.used)
+    if (lane + 64 * u < used)
       big = fmaxf(big, t.pM[base + (int64_t)(lane + 64 * u) * padded]);
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) big = fmaxf(big, __shfl_xor(big, o));
@@ -678,11 +1096,11 @@ __device__ __forceinline__ void join_row(const CacheView& c,
   float sum = 0.f;
   f32x4 x = {};
 #pragma unroll 4
-  for (int s = gr; s < pt.used; s += kGroups) {
+  for (int s = gr; s < used; s += kGroups) {
     const int64_t at = base + (int64_t)s * padded;
     const float m = t.pM[at], l = t.pL[at];
     const f32x4 o = *(const f32x4*)(t.pO + at * D + e);
-    const float f = m == neg_inf() ? 0.f : t.exp_of(m - big);
+    const float f = m == neg_inf() ? 0.f : exp2_(m - big);
     sum += f * l;
     x += f * o;
   }
@@ -721,16 +1139,6 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const CacheView c,
   join_row<P, D>(c, pl, t, blockIdx.x);
 }
 
-// What a key's weight becomes.
-__device__ __forceinline__ void add_weight(const CacheView& c,
-                                           const TreeCall& t, const Tree& tr,
-                                           int unit, int key, float mass) {
-  if (key < tr.len) {
-    float* w = c.weight + (int64_t)unit * c.cap + key;
-    *w = t.decay * *w + mass;
-  }
-}
-
 // Few rows (16 at most): their logits were stored, four keys a thread here.
 // The same launch joins the rows; the weights' work-groups take the rows'
 // sums from the splits themselves.
@@ -754,7 +1162,7 @@ __global__ __launch_bounds__(kThreads) void mass_stored_kernel(
   const Parts pt = parts_of(tr, t.k_new != nullptr, P::KT, pl.splits);
   const int tid = threadIdx.x;
   const int64_t key = key0 + 4 * tid;
-  const int padded = pl.row_blocks * 16 * pl.row_tiles;
+  const int padded = pl.padded;
   // sixteen threads a row
   {
     const int r = tid / 16, l16 = tid % 16;
@@ -764,7 +1172,7 @@ __global__ __launch_bounds__(kThreads) void mass_stored_kernel(
         m = t.row_m[(int64_t)unit * padded + r];
         cf = t.row_inv[(int64_t)unit * padded + r];
       } else {
-        const int64_t base = (int64_t)unit * pl.splits * padded + r;
+        const int64_t base = (int64_t)unit * pl.parts * padded + r;
         float pm[kMaxSplits / 16], sum = 0.f;
 #pragma unroll
         for (int u = 0; u < kMaxSplits / 16; ++u) {
@@ -778,7 +1186,7 @@ __global__ __launch_bounds__(kThreads) void mass_stored_kernel(
         for (int u = 0; u < kMaxSplits / 16; ++u) {
           const int s = l16 + 16 * u;
           if (s < pt.used)
-            sum += (pm[u] == neg_inf() ? 0.f : t.exp_of(pm[u] - m)) *
+            sum += (pm[u] == neg_inf() ? 0.f : exp2_(pm[u] - m)) *
                    t.pL[base + (int64_t)s * padded];
         }
 #pragma unroll
@@ -808,7 +1216,7 @@ __global__ __launch_bounds__(kThreads) void mass_stored_kernel(
       if (r < n_rows && coef[r] != 0.f)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          acc[i] += coef[r] * t.exp_of(x[r][i] - row_m[r]);
+          acc[i] += coef[r] * t.exp_of(x[r][i], row_m[r]);
     return acc;
   };
   if (key < tr.len) {
@@ -828,9 +1236,10 @@ __global__ __launch_bounds__(kThreads) void mass_stored_kernel(
 }
 
 // Many rows: the logits are formed again, 16 NK keys a wavefront, whose rows
-// stay in registers while the query rows pass by.
+// stay in registers while the query rows pass by in LDS, 128 at a time.
 template <class P>
 constexpr int kMassHalves = P::ES == 2 ? 4 : 2;
+constexpr int kMassRows = 128;
 
 template <class P, int D>
 __global__ __launch_bounds__(kThreads) void mass_kernel(const CacheView c,
@@ -838,20 +1247,23 @@ __global__ __launch_bounds__(kThreads) void mass_kernel(const CacheView c,
                                                         const TreeCall t,
                                                         int key_blocks) {
   constexpr int NK = kMassHalves<P>, TK = 16 * NK;
+  constexpr int RC = D * P::ES / 16;   // 16-byte chunks of a row
+  __shared__ __attribute__((aligned(16))) char qs[kMassRows * D * P::ES];
+  __shared__ float ref[kMassRows], coef[kMassRows];
   const int unit = blockIdx.x / key_blocks, kb = blockIdx.x % key_blocks;
   const int kvh = unit % c.hkv, seq = unit / c.hkv;
   const Tree tr = tree_of(c, t, seq);
   if (tr.n == 0) return;
   const int group = t.hq / c.hkv, n_rows = tr.n * group;
   constexpr int kWaves = kThreads / 64;
-  const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int tid = threadIdx.x, lane = tid & 63, c16 = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int cached = (tr.len + TK - 1) / TK;
+  const int drafts = t.w_new ? (tr.n + TK - 1) / TK : 0;
+  if (kb * kWaves >= cached + drafts) return;
   const int tile = kb * kWaves + wave;
-  const bool draft = tile >= cached;
+  const bool draft = tile >= cached, works = tile < cached + drafts;
   const int j0 = (tile - cached) * TK;
-  // (no barrier below: wavefronts without a tile leave)
-  if (draft && (j0 >= tr.n || !t.w_new)) return;
   typename P::Row k[NK];
   int n[NK];
   uint64_t anc = 0;
@@ -879,43 +1291,110 @@ __global__ __launch_bounds__(kThreads) void mass_kernel(const CacheView c,
       }
     }
   }
-  const int padded = pl.row_blocks * 16 * pl.row_tiles;
-  f32x4 acc[NK] = {};
-  for (int r0 = 0; r0 < n_rows; r0 += 16) {
-    const int r = min(r0 + c16, n_rows - 1), tok = r / group;
-    typename P::Row q;
-    P::load_row(q, t.q + ((int64_t)(tr.first + tok) * t.hq + kvh * group +
-                          r % group) * (D * P::ES) + 16 * g);
-    const float m = t.row_m[(int64_t)unit * padded + r];
-    float coef = t.row_inv[(int64_t)unit * padded + r];
-    const float vote = t.vote ? t.vote[tr.first + tok] : 1.f;
-    coef = vote == 0.f || r0 + c16 >= n_rows ? 0.f : coef * vote;
-    const uint64_t sees = draft ? __shfl(anc, tok) >> j0 : 0;
-#pragma unroll
-    for (int h = 0; h < NK; ++h) {
-      const f32x4 x = P::qk(k[h], q);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const bool see = !draft || (sees >> (16 * h + 4 * g + i) & 1);
-        if (coef != 0.f && see && 4 * g + i < n[h])
-          acc[h][i] += coef * t.exp_of(x[i] - m);
-      }
-    }
-  }
+  // keys of the lane that are there: bit 4h + i
+  uint32_t mine = 0;
 #pragma unroll
   for (int h = 0; h < NK; ++h)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 4; ++i)
+      if (4 * g + i < n[h]) mine |= 1u << (4 * h + i);
+  bool full = !draft;   // every row sees every key
 #pragma unroll
-      for (int o = 1; o < 16; o <<= 1) acc[h][i] += __shfl_xor(acc[h][i], o);
-      const int at = 16 * h + 4 * g + i;
-      if (c16 == 0) {
-        if (!draft)
-          add_weight(c, t, tr, unit, tile * TK + at, acc[h][i]);
-        else if (j0 + at < tr.n)
-          t.w_new[(int64_t)(tr.first + j0 + at) * c.hkv + kvh] = acc[h][i];
+  for (int h = 0; h < NK; ++h) full = full && n[h] == 16;
+  f32x4 acc[NK] = {};
+  // 16 query rows, from row r of the 128
+  auto take = [&](int r0, int r, auto all) {
+    typename P::Row q;
+    const int row = r + c16;
+#pragma unroll
+    for (int j = 0; j < P::KS; ++j)
+      __builtin_memcpy(&q.x[j],
+                       &qs[(row * RC + ((g + 4 * j) ^ (row & (RC >= 16 ? 15 : 7)))) * 16],
+                       16);
+    const float m = ref[row], cf = coef[row];
+    uint32_t see = mine;
+    if (!decltype(all)::value && draft) {
+      const uint64_t sees =
+          __shfl(anc, min(r0 + row, n_rows - 1) / group) >> j0;
+      see = 0;
+#pragma unroll
+      for (int h = 0; h < NK; ++h)
+        see |= ((uint32_t)(sees >> (16 * h + 4 * g)) & 15u) << (4 * h);
+      see &= mine;
+    }
+    // a row without weight: its logits may be anything
+    const bool counts = cf != 0.f;
+#pragma unroll
+    for (int h = 0; h < NK; ++h) {
+      const f32x4 s = P::qk(k[h], q);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float p = t.exp_of(s[i], m);
+        const bool add =
+            counts && (decltype(all)::value || (see >> (4 * h + i) & 1));
+        acc[h][i] = __builtin_fmaf(cf, add ? p : 0.f, acc[h][i]);
       }
     }
+  };
+  for (int r0 = 0; r0 < n_rows; r0 += kMassRows) {
+    const int rows = min(kMassRows, n_rows - r0), up = (rows + 15) & ~15;
+    if (r0) __syncthreads();
+    for (int u = tid; u < up * RC; u += kThreads) {
+      const int row = u / RC, ch = u % RC;
+      const int r = r0 + min(row, rows - 1), tok = r / group;
+      *(u32x4*)&qs[(row * RC + (ch ^ (row & (RC >= 16 ? 15 : 7)))) * 16] =
+          *(const u32x4*)(t.q + ((int64_t)(tr.first + tok) * t.hq +
+                                 kvh * group + r % group) * (D * P::ES) +
+                          16 * ch);
+    }
+    if (tid < up) {
+      const int r = r0 + min(tid, rows - 1);
+      const float inv = t.row_inv[(int64_t)unit * pl.padded + r];
+      const float vote = t.vote ? t.vote[tr.first + r / group] : 1.f;
+      ref[tid] = t.row_m[(int64_t)unit * pl.padded + r];
+      // (a vote of 0 keeps the row out, whatever it holds)
+      coef[tid] = vote == 0.f || tid >= rows ? 0.f : inv * vote;
+    }
+    __syncthreads();
+    if (!works) continue;
+    if (full)
+      for (int r = 0; r < up; r += 16) take(r0, r, Yes{});
+    else
+      for (int r = 0; r < up; r += 16) take(r0, r, No{});
+  }
+  if (!works) return;
+  // The sums over the 16 lanes of a key, each lane left with those of its own
+  // keys: at every step it passes on the half that is not.
+  constexpr int N = 4 * NK;
+  float v[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = acc[i / 4][i % 4];
+#pragma unroll
+  for (int o = 8, m = N / 2; o >= 1; o /= 2, m /= 2) {
+    const bool up = c16 & o;
+    if (m >= 1) {
+#pragma unroll
+      for (int i = 0; i < N / 2; ++i) {
+        if (i >= m) continue;
+        const float give = up ? v[i] : v[i + m];
+        v[i] = (up ? v[i + m] : v[i]) + __shfl_xor(give, o);
+      }
+    } else {
+      v[0] += __shfl_xor(v[0], o);
+    }
+  }
+  constexpr int kShare = 16 / N;   // lanes that hold the same sum
+  if (c16 % kShare) return;
+  const int e = c16 / kShare;      // 4h + i
+  const int at = 16 * (e / 4) + 4 * g + e % 4;
+  if (!draft) {
+    const int key = tile * TK + at;
+    if (key >= tr.len) return;
+    float* w = c.weight + (int64_t)unit * c.cap + key;
+    *w = t.decay * *w + v[0];
+  } else if (j0 + at < tr.n) {
+    t.w_new[(int64_t)(tr.first + j0 + at) * c.hkv + kvh] = v[0];
+  }
 }
 
 template <class P, int D>
@@ -926,7 +1405,10 @@ hipError_t launch_tree(const CacheView& c, const TreePlan& pl,
   if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
   const dim3 grid((unsigned)blocks), block(kThreads);
   const dim3 waves(64 * waves_of(pl.row_tiles));
-  if (pl.stored)
+  if (pl.wide) {
+    if constexpr (P::ES == 2)
+      tree_wide_kernel<P, D><<<grid, dim3(64 * kWideWaves), 0, s>>>(c, pl, t);
+  } else if (pl.stored)
     tree_kernel<P, D, 1, true><<<grid, waves, 0, s>>>(c, pl, t);
   else if (pl.row_tiles == 1)
     tree_kernel<P, D, 1, false><<<grid, waves, 0, s>>>(c, pl, t);
@@ -937,7 +1419,7 @@ hipError_t launch_tree(const CacheView& c, const TreePlan& pl,
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int64_t join =
-      pl.splits > 1 ? (int64_t)c.n_seq * c.hkv * pl.rows : 0;
+      pl.parts > 1 ? (int64_t)c.n_seq * c.hkv * pl.rows : 0;
   if (pl.stored) {
     const int kb = std::max(1, (t.max_len + 4 * kThreads - 1) / (4 * kThreads));
     const int64_t n = join + (int64_t)c.n_seq * c.hkv * kb;
@@ -969,21 +1451,34 @@ hipError_t launch_tree(const CacheView& c, const TreePlan& pl,
 TreePlan plan_tree(const CacheView& c, int32_t hq, int32_t max_tree,
                    int32_t max_len, int32_t accumulate) {
   TreePlan p{};
-  const int kt = c.fp32 ? 16 : 32;
   p.rows = hq / c.hkv * max_tree;
   p.row_tiles = p.rows <= 16 ? 1 : p.rows <= 32 || c.fp32 ? 2 : 4;
-  p.row_blocks = (p.rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles);
+  p.wide = !c.fp32 && p.rows > 64;
+  const int kt = p.wide ? kWideKeys : c.fp32 ? 16 : 32;
+  const int block = p.wide ? kWideBlock : 16 * p.row_tiles;
+  p.row_blocks = (p.rows + block - 1) / block;
+  p.padded = p.row_blocks * block;
   const int64_t tiles =
       ((int64_t)max_len + kt - 1) / kt + (max_tree + kt - 1) / kt;
-  // A sequence whose tiles its work-group passes in eight rounds is not split:
-  // that takes less than the second launch. Otherwise about 1,024 work-groups
-  // for the 256 CUs, two rounds a work-group at least.
-  const int w = waves_of(p.row_tiles);
   const int64_t units = (int64_t)c.n_seq * c.hkv * p.row_blocks;
-  int64_t splits = std::min<int64_t>(kMaxSplits, std::max<int64_t>(1, 1024 / units));
-  splits = std::min(splits, (tiles + 2 * w - 1) / (2 * w));
-  if (tiles <= 8 * w) splits = 1;
+  int64_t splits;
+  if (p.wide) {
+    // a work-group takes a CU: one round of them, four stages each at least
+    splits = std::max<int64_t>(1, 256 / units);
+    splits = std::min(splits, (tiles + 3) / 4);
+    splits = std::min<int64_t>(kMaxSplits / 2, splits);
+  } else {
+    // A sequence whose tiles its work-group passes in eight rounds is not
+    // split: that takes less than the second launch. Otherwise about 1,024
+    // work-groups for the 256 CUs, two rounds a work-group at least.
+    const int w = waves_of(p.row_tiles);
+    splits = std::max<int64_t>(1, 1024 / units);
+    splits = std::min(splits, (tiles + 2 * w - 1) / (2 * w));
+    splits = std::min<int64_t>(kMaxSplits, splits);
+    if (tiles <= 8 * w) splits = 1;
+  }
   p.splits = (int32_t)std::max<int64_t>(1, splits);
+  p.parts = p.wide ? 2 * p.splits : p.splits;
   p.stored = accumulate && p.rows <= kStoredRows;
   p.len_pad = ((int64_t)max_len + 31) / 32 * 32;
   size_t off = 0;
@@ -992,13 +1487,13 @@ TreePlan plan_tree(const CacheView& c, int32_t hq, int32_t max_tree,
     off += (bytes + 255) & ~size_t(255);
     return at;
   };
-  const size_t part = (size_t)c.n_seq * c.hkv * p.splits * p.row_blocks * 16 *
-                      p.row_tiles;
-  p.pO = take(p.splits > 1 ? part * c.d * 4 : 0);
-  p.pM = take(p.splits > 1 ? part * 4 : 0);
-  p.pL = take(p.splits > 1 ? part * 4 : 0);
-  p.row_m = take(accumulate ? part / p.splits * 4 : 0);
-  p.row_inv = take(accumulate ? part / p.splits * 4 : 0);
+  const size_t all = (size_t)c.n_seq * c.hkv * p.padded;   // rows
+  const size_t part = p.parts > 1 ? all * p.parts : 0;
+  p.pO = take(part * c.d * 4);
+  p.pM = take(part * 4);
+  p.pL = take(part * 4);
+  p.row_m = take(accumulate ? all * 4 : 0);
+  p.row_inv = take(accumulate ? all * 4 : 0);
   p.score = take(p.stored ? (size_t)c.n_seq * c.hkv * p.rows *
                                 (p.len_pad + kMaxTree) * 4
                           : 0);
