@@ -415,7 +415,8 @@ evisel_status evisel_cache_append(const evisel_cache* cache,
  * (at most 64; none leaves the sequence alone); each sees every cached
  * token of its sequence, itself, and its ancestors among the drafted ones.
  * One token per sequence is ordinary generation.
- *   q         device [n_tok, hq, d], the cache's dtype
+ *   q         device [n_tok, hq, d], the cache's dtype; hq a multiple of
+ *             hkv, at most 4096 times it
  *   k_new, v_new  device [n_tok, hkv, d]: the drafted tokens' own keys and
  *             values, or both NULL: the tokens see the cache alone (which
  *             already holds what they are to see)

@@ -110,6 +110,12 @@ struct TreeCall {
   float* row_inv;            // reference and 1 / sum (accumulate)
   float* score;              // [seq][kv head][row][len_pad + 64] q.k
 
+  // The token of a query row: r / group by a multiplication with 2^32 / group
+  // rounded up, exact as r * group < 2^32 (0: a group of one).
+  uint32_t group_inv;
+  __device__ __forceinline__ int token_of(int r) const {
+    return group_inv ? (int)__umulhi((uint32_t)r, group_inv) : r;
+  }
   // exp2 of a logit (as q.k) over a reference (log2 units). One rounding, of
   // a value that is small where it matters; the reference's own cancels.
   __device__ __forceinline__ float exp_of(float x, float ref) const {

@@ -157,44 +157,66 @@ hipError_t launch_append(const CacheView& c, const AppendCall& a,
 // ---------------------------------------------------------------------------
 // Evict.
 
-// Kept tokens rank by this: larger first. Tokens that are always kept lead,
-// NaN ranks like -inf, and -0 like 0.
+// Kept tokens rank by this: larger first. Tokens that are always kept (those
+// of positions outside n_sink .. n_sink + span - 1) lead, NaN ranks like -inf,
+// and -0 like 0.
 __device__ __forceinline__ uint32_t keep_key(float w, int pos, int n_sink,
-                                             int64_t recent_from) {
-  if (pos < n_sink || pos >= recent_from) return 0xFFFFFFFFu;
-  uint32_t b = __float_as_uint(w);
-  if (w != w) b = 0xFF800000u;
-  if (b == 0x80000000u) b = 0u;
-  return b & 0x80000000u ? ~b : b | 0x80000000u;
+                                             uint32_t span) {
+  const int b = (int)__float_as_uint(w + 0.f);   // -0 + 0 = 0
+  uint32_t k = (uint32_t)(b ^ ((b >> 31) | (int)0x80000000));
+  if (w != w) k = 0x007FFFFFu;
+  return (uint32_t)pos - (uint32_t)n_sink >= span ? 0xFFFFFFFFu : k;
+}
+// Which of slots i .. i + 3 lie below `end`, as bits.
+__device__ __forceinline__ uint32_t below4(int i, int end) {
+  return (1u << min(max(end - i, 0), 4)) - 1;
 }
 
 constexpr int kEvThreads = 1024;
 constexpr int kEvWaves = kEvThreads / 64;
 constexpr int kEvBins = 2048;
-// keys that stay in LDS (the kernel's other arrays take 25 KB of the 160)
-constexpr int kEvLdsKeys = 32 * 1024;
-
-// keys of one digit's bin that stay in LDS as a list
+// Histograms side by side, lane by lane: equal weights are 16 additions to one
+// place and not 64, and the four neighbours lie in different banks.
+constexpr int kEvCopies = 4;
+// keys of one digit's bin that are kept as a list, with their slots
 constexpr int kEvList = 4096;
+// keys that stay in LDS (the kernel's other arrays take 65 KB of the 160)
+constexpr int kEvLdsKeys = 23 * 1024;
+
+// Sum over the lanes before this one, and over all (wave-uniform).
+__device__ __forceinline__ uint32_t lanes_before(uint32_t x, int lane,
+                                                 uint32_t* all) {
+  uint32_t run = x;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint32_t up = __shfl_up(run, o);
+    if (lane >= o) run += up;
+  }
+  *all = __builtin_amdgcn_readlane(run, 63);
+  return run - x;
+}
 
 // One work-group per sequence and kv head: which slots it keeps, and from
-// that the moves. The budget-th largest key comes digit by digit (11, 11 and
-// 10 bits, a histogram each): the first digit from every key, the others, as a
-// rule, from the short list of keys that share the digits before; equal keys
-// are kept from the lowest slot on. Then every wavefront walks its own run of
-// slots twice, 256 at a time: counting, and, with what the runs before it
-// counted, writing the holes below the budget and the kept slots above it into
-// the two lists. LDS: the keys stay in LDS between the passes; otherwise each
-// pass makes them again from weight and pos.
+// that the moves. The budget-th largest key comes digit by digit, 11, 11 and
+// 10 bits, a histogram each. The first takes every key; a second pass, in
+// which every wavefront has a run of slots to itself, counts the run's keys
+// above that digit and lists those that have it, and the rest works on that
+// list (on all keys, if they are too many). Equal keys are kept from the
+// lowest slot on. The third pass knows how many holes and kept tail slots the
+// runs before hold and writes its own into the two lists, 256 slots at a time.
+// LDS: the keys stay there between the passes; otherwise each pass makes them
+// again from weight and pos.
 template <bool LDS>
 __global__ __launch_bounds__(kEvThreads) void evict_select_kernel(
     const CacheView c, const EvictCall e) {
-  __shared__ uint32_t hist[kEvBins];
-  __shared__ uint32_t list[kEvList];
+  __shared__ uint32_t hist[kEvBins * kEvCopies];
+  __shared__ uint32_t list_key[kEvList];
+  __shared__ int list_slot[kEvList];
   __shared__ uint32_t wave_tot[kEvWaves];
   __shared__ uint32_t found[2];          // the digit, and what is above it
   __shared__ uint32_t listed;
-  __shared__ int runs[kEvWaves][4];      // above / equal, below / from budget
+  // of a wavefront's run: keys above and equal, below the budget and from it
+  __shared__ int runs[4][kEvWaves];
   extern __shared__ __attribute__((aligned(16))) uint32_t keys[];
   const int unit = blockIdx.x, seq = unit / c.hkv;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -204,7 +226,8 @@ __global__ __launch_bounds__(kEvThreads) void evict_select_kernel(
     if (tid == 0) e.count[unit] = 0;
     return;
   }
-  const int64_t recent_from = (int64_t)c.seen[seq] - e.n_recent;
+  const uint32_t span = (uint32_t)max(
+      (int64_t)0, (int64_t)c.seen[seq] - e.n_recent - e.n_sink);
   const float* w = c.weight + (int64_t)unit * c.cap;
   const int32_t* pos = c.pos + (int64_t)unit * c.cap;
   // Keys i .. i + 3 (i a multiple of 4; the capacity is one of 16, so that
@@ -215,243 +238,262 @@ __global__ __launch_bounds__(kEvThreads) void evict_select_kernel(
     u32x4 k;
 #pragma unroll
     for (int u = 0; u < 4; ++u)
-      k[u] = keep_key(x[u], p[u], e.n_sink, recent_from);
+      k[u] = keep_key(x[u], p[u], e.n_sink, span);
     return k;
   };
   auto four = [&](int i) {
     return LDS ? *(const u32x4*)(keys + i) : make(i);
   };
-  // One key a lane into the histogram. The bin of the first lane that has one
-  // is added at once, so that a run of equal weights is no chain of additions
-  // to one place.
-  auto count = [&](bool in, uint32_t bin) {
-    const uint64_t active = __ballot(in);
-    if (!active) return;
-    const int lead = __builtin_ctzll(active);
-    const uint32_t b0 = __builtin_amdgcn_readlane(bin, lead);
-    const uint64_t same = __ballot(in && bin == b0);
-    if (lane == lead) atomicAdd(&hist[b0], (uint32_t)__popcll(same));
-    if (in && bin != b0) atomicAdd(&hist[bin], 1u);
+  auto count = [&](uint32_t bin) {
+    atomicAdd(&hist[bin * kEvCopies + lane % kEvCopies], 1u);
   };
   auto clear = [&] {
-    for (int i = tid; i < kEvBins; i += kEvThreads) hist[i] = 0;
-    if (tid == 0) listed = 0;
+    for (int i = 4 * tid; i < kEvBins * kEvCopies; i += 4 * kEvThreads)
+      *(u32x4*)(hist + i) = u32x4{};
     __syncthreads();
   };
   // The bin, from the largest down, in which the running count reaches
   // `need`: found[0], and the count above it: found[1]. Two bins a thread.
   auto locate = [&](uint32_t need) {
     __syncthreads();
-    const uint32_t c0 = hist[kEvBins - 1 - 2 * tid];
-    const uint32_t c1 = hist[kEvBins - 2 - 2 * tid];
-    uint32_t run = c0 + c1;
+    uint32_t n[2];
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const uint32_t up = __shfl_up(run, o);
-      if (lane >= o) run += up;
+    for (int u = 0; u < 2; ++u) {
+      static_assert(kEvCopies == 4, "one read a bin");
+      const u32x4 h = *(const u32x4*)(hist + (kEvBins - 1 - 2 * tid - u) * 4);
+      n[u] = h[0] + h[1] + h[2] + h[3];
     }
-    if (lane == 63) wave_tot[wave] = run;
+    uint32_t all;
+    uint32_t before = lanes_before(n[0] + n[1], lane, &all);
+    if (lane == 0) wave_tot[wave] = all;
     __syncthreads();
-    uint32_t before = run - c0 - c1;
-    for (int i = 0; i < wave; ++i) before += wave_tot[i];
-    if (before < need && before + c0 >= need) {
+    uint32_t t = lane < wave ? wave_tot[lane] : 0u;   // (16 wavefronts)
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) t += __shfl_xor(t, o);
+    before += __builtin_amdgcn_readfirstlane(t);
+    if (before < need && before + n[0] >= need) {
       found[0] = kEvBins - 1 - 2 * tid;
       found[1] = before;
-    } else if (before + c0 < need && before + c0 + c1 >= need) {
+    } else if (before + n[0] < need && before + n[0] + n[1] >= need) {
       found[0] = kEvBins - 2 - 2 * tid;
-      found[1] = before + c0;
+      found[1] = before + n[0];
     }
     __syncthreads();
   };
   constexpr int kStep = 4 * kEvThreads;
 
   // first digit
+  if (tid == 0) listed = 0;
+  if (tid < 4 * kEvWaves) runs[tid / kEvWaves][tid % kEvWaves] = 0;
   clear();
 #pragma unroll 2
-  for (int i0 = 0; i0 < len; i0 += kStep) {
-    const int i = i0 + 4 * tid;
-    u32x4 k = {};
-    if (i < len) {
-      k = make(i);
-      if (LDS) *(u32x4*)(keys + i) = k;
-    }
+  for (int i = 4 * tid; i < len; i += kStep) {
+    const u32x4 k = make(i);
+    if (LDS) *(u32x4*)(keys + i) = k;
+    if (i + 4 <= len) {
 #pragma unroll
-    for (int u = 0; u < 4; ++u) count(i + u < len, k[u] >> 21);
+      for (int u = 0; u < 4; ++u) count(k[u] >> 21);
+    } else {
+      for (int u = 0; u < (len & 3); ++u)
+        count((u == 0 ? k[0] : u == 1 ? k[1] : k[2]) >> 21);
+    }
   }
   uint32_t need = (uint32_t)e.budget;   // keys still wanted among the matching
   locate(need);
-  uint32_t prefix = found[0] << 21;
+  const uint32_t digit = found[0];
+  uint32_t prefix = digit << 21;
   need -= found[1];
-  // the keys that share it, into the list (or, if they are too many, again
-  // from all keys), and their second digit
-  clear();
+
+  // the keys that have it
+  const int per = ((len + 256 * kEvWaves - 1) / (256 * kEvWaves)) * 256;
+  const int a = min(wave * per, len), b = min(a + per, len);
+  {
+    int lo = 0, hi = 0;   // keys above, by side of the budget
 #pragma unroll 2
-  for (int i0 = 0; i0 < len; i0 += kStep) {
-    const int i = i0 + 4 * tid;
-    u32x4 k = {};
-    if (i < len) k = four(i);
+    for (int i = a + 4 * lane; i < b; i += 256) {
+      const u32x4 k = four(i);
+      uint32_t gt = 0, eq = 0;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const bool in = i + u < len && (k[u] & 0xFFE00000u) == prefix;
-      const uint64_t m = __ballot(in);
-      if (!m) continue;
-      const int lead = __builtin_ctzll(m);
-      uint32_t at = 0;
-      if (lane == lead) at = atomicAdd(&listed, (uint32_t)__popcll(m));
-      at = __builtin_amdgcn_readlane(at, lead) +
-           (uint32_t)__popcll(m & ((1ull << lane) - 1));
-      if (in && at < kEvList) list[at] = k[u];
-      count(in, (k[u] >> 10) & 2047u);
+      for (int u = 0; u < 4; ++u) {
+        const uint32_t top = k[u] >> 21;
+        gt |= (uint32_t)(top > digit) << u;
+        eq |= (uint32_t)(top == digit) << u;
+      }
+      const uint32_t in = below4(i, b), low = below4(i, e.budget);
+      gt &= in;
+      lo += __popc(gt & low);
+      hi += __popc(gt & ~low);
+      for (eq &= in; eq; eq &= eq - 1) {
+        const int u = __builtin_ctz(eq);
+        const uint32_t at = atomicAdd(&listed, 1u);
+        if (at < kEvList) {
+          list_key[at] = u < 2 ? (u ? k[1] : k[0]) : (u == 3 ? k[3] : k[2]);
+          list_slot[at] = i + u;
+        }
+      }
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      lo += __shfl_xor(lo, o);
+      hi += __shfl_xor(hi, o);
+    }
+    if (lane == 0) {
+      runs[0][wave] = lo;
+      runs[2][wave] = hi;
     }
   }
+  clear();
+  const int n_list = (int)listed;
+  const bool whole = n_list > kEvList;   // too many: all keys again
+  // f(key, slot) for every key that may still matter
+  auto each = [&](auto f) {
+    if (!whole) {
+      for (int i = tid; i < n_list; i += kEvThreads)
+        f(list_key[i], list_slot[i]);
+    } else {
+      for (int i = 4 * tid; i < len; i += kStep) {
+        const u32x4 k = four(i);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (i + u < len && k[u] >> 21 == digit)
+            f(k[u], i + u);
+      }
+    }
+  };
+  each([&](uint32_t k, int) { count((k >> 10) & 2047u); });
   locate(need);
   prefix |= found[0] << 10;
   need -= found[1];
-  const uint32_t n_list = listed;
-  __syncthreads();   // every thread has read `listed`
   clear();
-  if (n_list <= kEvList) {
-    for (uint32_t i0 = 0; i0 < n_list; i0 += kEvThreads) {
-      const uint32_t i = i0 + tid, k = i < n_list ? list[i] : 0u;
-      count(i < n_list && (k & 0xFFFFFC00u) == prefix, k & 1023u);
-    }
-  } else {
-    for (int i0 = 0; i0 < len; i0 += kStep) {
-      const int i = i0 + 4 * tid;
-      u32x4 k = {};
-      if (i < len) k = four(i);
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-        count(i + u < len && (k[u] & 0xFFFFFC00u) == prefix, k[u] & 1023u);
-    }
-  }
+  each([&](uint32_t k, int) {
+    if ((k & 0xFFFFFC00u) == prefix) count(k & 1023u);
+  });
   locate(need);
   prefix |= found[0];
   need -= found[1];
   // kept: keys above `prefix`, and the first `need` that equal it
-
-  const int per = ((len + 256 * kEvWaves - 1) / (256 * kEvWaves)) * 256;
-  const int a = min(wave * per, len), b = min(a + per, len);
-  int n_gt[2] = {0, 0}, n_eq[2] = {0, 0};
-#pragma unroll 2
-  for (int i0 = a; i0 < b; i0 += 256) {
-    const int i = i0 + 4 * lane;
-    u32x4 k = {};
-    if (i < b) k = four(i);
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const bool in = i + u < b, hi = i + u >= e.budget;
-      const bool gt = in && k[u] > prefix, eq = in && k[u] == prefix;
-      n_gt[0] += gt && !hi;
-      n_gt[1] += gt && hi;
-      n_eq[0] += eq && !hi;
-      n_eq[1] += eq && hi;
-    }
-  }
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    n_gt[0] += __shfl_xor(n_gt[0], o);
-    n_gt[1] += __shfl_xor(n_gt[1], o);
-    n_eq[0] += __shfl_xor(n_eq[0], o);
-    n_eq[1] += __shfl_xor(n_eq[1], o);
-  }
-  if (lane == 0) {
-    runs[wave][0] = n_gt[0];
-    runs[wave][1] = n_eq[0];
-    runs[wave][2] = n_gt[1];
-    runs[wave][3] = n_eq[1];
-  }
+  each([&](uint32_t k, int slot) {
+    if (k >= prefix)
+      atomicAdd(&runs[2 * (slot >= e.budget) + (k == prefix)][slot / per], 1);
+  });
   __syncthreads();
+
   // what the runs before this one hold: equal keys, holes, kept tail slots
-  int eqs = 0, holes = 0, tails = 0;
-  for (int u = 0; u < wave; ++u) {
+  int eqs = 0, holes = 0, tails = 0, all_eq = 0;
+#pragma unroll
+  for (int u = 0; u < kEvWaves; ++u) {
     const int ua = min(u * per, len), ub = min(ua + per, len);
     const int below = max(0, min(ub, e.budget) - ua);
-    const int k0 = min(max((int)need - eqs, 0), runs[u][1]);
-    eqs += runs[u][1];
-    const int k1 = min(max((int)need - eqs, 0), runs[u][3]);
-    eqs += runs[u][3];
-    holes += below - runs[u][0] - k0;
-    tails += runs[u][2] + k1;
+    const int e0 = runs[1][u], e1 = runs[3][u];
+    const int k0 = min(max((int)need - all_eq, 0), e0);
+    const int k1 = min(max((int)need - all_eq - e0, 0), e1);
+    all_eq += e0 + e1;
+    if (u < wave) {
+      eqs = all_eq;
+      holes += below - runs[0][u] - k0;
+      tails += runs[2][u] + k1;
+    }
   }
   int32_t* to = e.to + (int64_t)unit * e.max_moves;
   int32_t* from = e.from + (int64_t)unit * e.max_moves;
-  const uint64_t below_lane = (1ull << lane) - 1;
+  const bool ties = all_eq > (int)need;   // some equal keys go
 #pragma unroll 2
   for (int i0 = a; i0 < b; i0 += 256) {
     const int i = i0 + 4 * lane;
     u32x4 k = {};
     if (i < b) k = four(i);
     // slots in order: lane by lane, each its four
-    int before = eqs;
-    bool eq[4], kept[4], out[4];
+    uint32_t keep = 0, same = 0;
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      eq[u] = i + u < b && k[u] == prefix;
-      const uint64_t m = __ballot(eq[u]);
-      before += __popcll(m & below_lane);
-      eqs += __popcll(m);
+      keep |= (uint32_t)(k[u] >= prefix) << u;
+      same |= (uint32_t)(k[u] == prefix) << u;
     }
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      kept[u] = i + u < b &&
-                (k[u] > prefix || (eq[u] && before < (int)need));
-      before += eq[u];
+    const uint32_t in = below4(i, b), low = below4(i, e.budget);
+    keep &= in;
+    if (ties) {
+      same &= in;
+      uint32_t all;
+      int left = (int)need - eqs -
+                 (int)lanes_before((uint32_t)__popc(same), lane, &all);
+      eqs += (int)all;
+      for (; same; same &= same - 1)
+        if (left-- <= 0) keep &= ~(same & -same);
     }
-    int hole = holes, tail = tails;
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const bool hi = i + u >= e.budget;
-      out[u] = i + u < b && !hi && !kept[u];
-      kept[u] = kept[u] && hi;
-      const uint64_t mh = __ballot(out[u]), mt = __ballot(kept[u]);
-      hole += __popcll(mh & below_lane);
-      tail += __popcll(mt & below_lane);
-      holes += __popcll(mh);
-      tails += __popcll(mt);
-    }
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      if (out[u]) to[hole++] = i + u;
-      if (kept[u]) from[tail++] = i + u;
-    }
+    uint32_t out = in & low & ~keep, tail = keep & ~low;
+    uint32_t all;
+    const uint32_t at = lanes_before(
+        (uint32_t)__popc(out) | (uint32_t)__popc(tail) << 16, lane, &all);
+    int h = holes + (int)(at & 0xFFFFu), s = tails + (int)(at >> 16);
+    for (; out; out &= out - 1) to[h++] = i + __builtin_ctz(out);
+    for (; tail; tail &= tail - 1) from[s++] = i + __builtin_ctz(tail);
+    holes += (int)(all & 0xFFFFu);
+    tails += (int)(all >> 16);
   }
   if (wave == kEvWaves - 1 && lane == 0) e.count[unit] = tails;
 }
 
-// The moves: RC lanes copy a row of K and of V. A slot from the budget on is
-// never written, so no move waits for another. The first work-group of a
-// sequence's first head sets its length: nothing here reads that.
+// The moves: RC lanes copy a row of K and of V, kMvRows rows each, all on
+// their way at once. A slot from the budget on is never written, so no move
+// waits for another. The first work-group of a sequence's first head sets its
+// length: nothing here reads that.
 constexpr int kMvThreads = 256;
+constexpr int kMvRows = 4;
 template <int RC>
 __global__ __launch_bounds__(kMvThreads) void evict_move_kernel(
-    const CacheView c, const EvictCall e, int per_block, int blocks_per_unit) {
+    const CacheView c, const EvictCall e, int blocks_per_unit) {
+  constexpr int kStep = kMvThreads / RC;
   const int unit = blockIdx.x / blocks_per_unit;
   const int part = blockIdx.x % blocks_per_unit;
   const int seq = unit / c.hkv, h = unit % c.hkv;
   if (part == 0 && h == 0 && threadIdx.x == 0 &&
       c.length[seq] > e.budget)
     c.length[seq] = e.budget;
-  const int n = min(e.count[unit], (part + 1) * per_block);
+  const int n = e.count[unit];
+  const int ch = threadIdx.x % RC;
+  const int i0 = part * kMvRows * kStep + (int)threadIdx.x / RC;
+  if (i0 >= n) return;
   const int32_t* to = e.to + (int64_t)unit * e.max_moves;
   const int32_t* from = e.from + (int64_t)unit * e.max_moves;
-  const int ch = threadIdx.x % RC;
-  for (int i = part * per_block + (int)threadIdx.x / RC; i < n;
-       i += kMvThreads / RC) {
-    const int src = from[i], dst = to[i];
-    const int64_t so = slot_offset(c, seq, src);
-    const int64_t dp = slot_offset(c, seq, dst);
-    const int64_t at = h * c.head_bytes + 16 * ch;
-    if (so >= 0 && dp >= 0) {
-      const i32x4 k = *(const i32x4*)(c.k + so + at);
-      const i32x4 v = *(const i32x4*)(c.v + so + at);
-      *(i32x4*)(c.k + dp + at) = k;
-      *(i32x4*)(c.v + dp + at) = v;
+  const int64_t at = h * c.head_bytes + 16 * ch, row = (int64_t)unit * c.cap;
+  int src[kMvRows], dst[kMvRows];
+  int64_t so[kMvRows], dp[kMvRows];
+  i32x4 k[kMvRows], v[kMvRows];
+#pragma unroll
+  for (int u = 0; u < kMvRows; ++u) {   // (past the end: the first again)
+    const int i = i0 + u * kStep < n ? i0 + u * kStep : i0;
+    src[u] = from[i];
+    dst[u] = to[i];
+  }
+#pragma unroll
+  for (int u = 0; u < kMvRows; ++u) {
+    so[u] = slot_offset(c, seq, src[u]);
+    dp[u] = slot_offset(c, seq, dst[u]);
+  }
+#pragma unroll
+  for (int u = 0; u < kMvRows; ++u)
+    if (so[u] >= 0) {
+      k[u] = *(const i32x4*)(c.k + so[u] + at);
+      v[u] = *(const i32x4*)(c.v + so[u] + at);
+    }
+  float w[kMvRows];
+  int32_t p[kMvRows];
+  if (ch == 0)
+#pragma unroll
+    for (int u = 0; u < kMvRows; ++u) {
+      w[u] = c.weight[row + src[u]];
+      p[u] = c.pos[row + src[u]];
+    }
+#pragma unroll
+  for (int u = 0; u < kMvRows; ++u) {
+    if (u && i0 + u * kStep >= n) break;
+    if (so[u] >= 0 && dp[u] >= 0) {
+      *(i32x4*)(c.k + dp[u] + at) = k[u];
+      *(i32x4*)(c.v + dp[u] + at) = v[u];
     }
     if (ch == 0) {
-      const int64_t row = (int64_t)unit * c.cap;
-      c.weight[row + dst] = c.weight[row + src];
-      c.pos[row + dst] = c.pos[row + src];
+      c.weight[row + dst[u]] = w[u];
+      c.pos[row + dst[u]] = p[u];
     }
   }
 }
@@ -459,11 +501,11 @@ __global__ __launch_bounds__(kMvThreads) void evict_move_kernel(
 template <int RC>
 hipError_t launch_move(const CacheView& c, const EvictCall& e, hipStream_t s) {
   const int units = c.n_seq * c.hkv;
-  const int per = 4 * kMvThreads / RC;   // four rows per thread
+  const int per = kMvRows * kMvThreads / RC;
   const int64_t parts = (e.max_moves + per - 1) / per;
   if (parts * units > 0x7FFFFFFF) return hipErrorInvalidValue;
   evict_move_kernel<RC><<<dim3((unsigned)(parts * units)), dim3(kMvThreads), 0,
-                          s>>>(c, e, per, (int)parts);
+                          s>>>(c, e, (int)parts);
   return hipGetLastError();
 }
 
@@ -483,7 +525,7 @@ hipError_t launch_cache_evict(const CacheView& c, const EvictCall& e,
   if ((int64_t)c.n_seq * c.hkv > 0x7FFFFFFF) return hipErrorInvalidValue;
   if (e.max_len <= kEvLdsKeys) {
     const size_t lds = ((size_t)e.max_len * 4 + 15) & ~size_t(15);
-    if (lds + 32 * 1024 > 64 * 1024) {
+    if (lds > 0) {   // with the static arrays past 64 KB
       const hipError_t r = hipFuncSetAttribute(
           (const void*)evict_select_kernel<true>,
           hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);

@@ -88,9 +88,13 @@ size_t evict_layout(const evisel::CacheView& c, int32_t budget,
   return align256(n * 4) + 2 * lists;
 }
 
+// Query heads of a kv head (the kernels' division by it is exact up to 2^13).
+constexpr int kMaxGroup = 4096;
+
 bool tree_bounds(const evisel::CacheView& c, int32_t hq, int32_t max_tree,
                  int32_t max_len) {
-  return hq >= 1 && hq % c.hkv == 0 && hq <= 1 << 14 && max_tree >= 1 &&
+  return hq >= 1 && hq % c.hkv == 0 && hq / c.hkv <= kMaxGroup &&
+         max_tree >= 1 &&
          max_tree <= 64 && max_len >= 0 && max_len <= c.cap;
 }
 
@@ -152,8 +156,8 @@ evisel_status evisel_tree_attention(
   const evisel_status st = check_cache(cache, &c);
   if (st != EVISEL_OK) return st;
   if (!tree_bounds(c, hq, max_tree, max_len))
-    return bad("need hq a multiple of hkv, 1 <= max_tree <= 64 and "
-               "0 <= max_len <= capacity");
+    return bad("need hq a multiple of hkv (at most 4096 times it), "
+               "1 <= max_tree <= 64 and 0 <= max_len <= capacity");
   if (n_tok < 0) return bad("negative n_tok");
   if (!tree_ptr) return bad("null tree_ptr");
   if ((k_new == nullptr) != (v_new == nullptr))
@@ -191,6 +195,8 @@ evisel_status evisel_tree_attention(
   t.vote = accumulate ? vote : nullptr;
   t.w_new = accumulate ? w_new : nullptr;
   t.scale_log2 = softmax_scale * 1.4426950408889634f;
+  const uint32_t group = (uint32_t)(hq / c.hkv);
+  t.group_inv = group == 1 ? 0u : (uint32_t)(0xFFFFFFFFu / group) + 1u;
   t.decay = decay;
   t.hq = hq;
   t.n_tok = n_tok;

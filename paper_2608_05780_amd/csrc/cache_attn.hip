@@ -451,7 +451,7 @@ __device__ __forceinline__ void take_drafts(Rows<P, D, RT>& rows,
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const int r = row0 + 16 * rt + c16;
-    const uint64_t all = __shfl(anc, min(r, n_rows - 1) / group);
+    const uint64_t all = __shfl(anc, t.token_of(min(r, n_rows - 1)));
     sees[rt] = r < n_rows ? (uint32_t)(all >> j0) : 0u;
     vis[rt] = 0;
 #pragma unroll
@@ -551,7 +551,7 @@ __global__ __launch_bounds__(64 * waves_of(RT), RT == 4 ? 1 : 2) void tree_kerne
 #pragma unroll
     for (int i = 0; i < P::NT; ++i) rows.o[rt][i] = f32x4{};
     if (r < n_rows) {
-      const int tok = r / group, qh = r % group;
+      const int tok = t.token_of(r), qh = r - tok * group;
       P::load_row(rows.q[rt],
                   t.q + ((int64_t)(tr.first + tok) * t.hq + kvh * group + qh) *
                             (D * P::ES) + 16 * g);
@@ -671,7 +671,7 @@ __global__ __launch_bounds__(64 * waves_of(RT), RT == 4 ? 1 : 2) void tree_kerne
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
         for (int i = 0; i < kCols; ++i) x[i] *= inv;
-        const int tok = r / group, h = kvh * group + r % group;
+        const int tok = t.token_of(r), h = kvh * group + r - tok * group;
         P::template store<kCols>(
             t.out + ((int64_t)(tr.first + tok) * t.hq + h) * (D * P::ES) +
                 ec * kCols * P::ES, x);
@@ -750,7 +750,7 @@ __global__ __launch_bounds__(64 * kWideWaves, kWideRt == 2 ? 2 : 1) void tree_wi
 #pragma unroll
     for (int i = 0; i < NT; ++i) rows.o[rt][i] = f32x4{};
     if (r < n_rows) {
-      const int tok = r / group, qh = r % group;
+      const int tok = t.token_of(r), qh = r - tok * group;
       P::load_row(rows.q[rt],
                   t.q + ((int64_t)(tr.first + tok) * t.hq + kvh * group + qh) *
                             (D * P::ES) + 16 * g);
@@ -979,7 +979,7 @@ __global__ __launch_bounds__(64 * kWideWaves, kWideRt == 2 ? 2 : 1) void tree_wi
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
           const int r = row0 + 16 * rt + c16;
-          const uint64_t all = __shfl(anc, min(r, n_rows - 1) / group);
+          const uint64_t all = __shfl(anc, t.token_of(min(r, n_rows - 1)));
           sees[rt] = r < n_rows ? (uint32_t)(all >> (KT * sub)) : 0u;
           vis[rt] = 0;
 #pragma unroll
@@ -1042,7 +1042,7 @@ __global__ __launch_bounds__(64 * kWideWaves, kWideRt == 2 ? 2 : 1) void tree_wi
       continue;
     }
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    const int tok = r / group, h = kvh * group + r % group;
+    const int tok = t.token_of(r), h = kvh * group + r - tok * group;
     char* dst = t.out + (((int64_t)(tr.first + tok) * t.hq + h) * D +
                          D / 4 * g) * P::ES;
 #pragma unroll
@@ -1117,7 +1117,7 @@ __device__ __forceinline__ void join_row(const CacheView& c,
   }
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   x *= inv;
-  const int tok = r / group, h = kvh * group + r % group;
+  const int tok = t.token_of(r), h = kvh * group + r - tok * group;
   char* dst = t.out + (((int64_t)(tr.first + tok) * t.hq + h) * D + e) * P::ES;
   if constexpr (P::ES == 2)
     *(bf16x4*)dst = __builtin_convertvector(x, bf16x4);
@@ -1193,7 +1193,7 @@ __global__ __launch_bounds__(kThreads) void mass_stored_kernel(
         for (int o = 1; o < 16; o <<= 1) sum += __shfl_xor(sum, o);
         cf = sum == 0.f ? 0.f : 1.f / sum;
       }
-      const float vote = t.vote ? t.vote[tr.first + r / group] : 1.f;
+      const float vote = t.vote ? t.vote[tr.first + t.token_of(r)] : 1.f;
       // (a vote of 0 keeps the row out, whatever it holds)
       cf = vote == 0.f ? 0.f : cf * vote;
     }
@@ -1315,7 +1315,7 @@ __global__ __launch_bounds__(kThreads) void mass_kernel(const CacheView c,
     uint32_t see = mine;
     if (!decltype(all)::value && draft) {
       const uint64_t sees =
-          __shfl(anc, min(r0 + row, n_rows - 1) / group) >> j0;
+          __shfl(anc, t.token_of(min(r0 + row, n_rows - 1))) >> j0;
       see = 0;
 #pragma unroll
       for (int h = 0; h < NK; ++h)
@@ -1341,16 +1341,16 @@ __global__ __launch_bounds__(kThreads) void mass_kernel(const CacheView c,
     if (r0) __syncthreads();
     for (int u = tid; u < up * RC; u += kThreads) {
       const int row = u / RC, ch = u % RC;
-      const int r = r0 + min(row, rows - 1), tok = r / group;
+      const int r = r0 + min(row, rows - 1), tok = t.token_of(r);
       *(u32x4*)&qs[(row * RC + (ch ^ (row & (RC >= 16 ? 15 : 7)))) * 16] =
           *(const u32x4*)(t.q + ((int64_t)(tr.first + tok) * t.hq +
-                                 kvh * group + r % group) * (D * P::ES) +
-                          16 * ch);
+                                 kvh * group + r - tok * group) *
+                                    (D * P::ES) + 16 * ch);
     }
     if (tid < up) {
       const int r = r0 + min(tid, rows - 1);
       const float inv = t.row_inv[(int64_t)unit * pl.padded + r];
-      const float vote = t.vote ? t.vote[tr.first + r / group] : 1.f;
+      const float vote = t.vote ? t.vote[tr.first + t.token_of(r)] : 1.f;
       ref[tid] = t.row_m[(int64_t)unit * pl.padded + r];
       // (a vote of 0 keeps the row out, whatever it holds)
       coef[tid] = vote == 0.f || tid >= rows ? 0.f : inv * vote;

@@ -123,7 +123,7 @@ def test_valid_views(lib):
 
 def test_attention_arguments(lib):
     I, W = ev.ERR_INVALID_ARG, ev.ERR_WORKSPACE
-    for kw in (dict(hq=3), dict(hq=0), dict(hq=1 << 15), dict(max_tree=0),
+    for kw in (dict(hq=3), dict(hq=0), dict(hq=2 * 4097), dict(max_tree=0),
                dict(max_tree=65), dict(max_len=-1), dict(max_len=65),
                dict(n_tok=-1), dict(tree_ptr=None), dict(k_new=None),
                dict(v_new=None), dict(scale=0.0), dict(scale=float("nan")),
