@@ -82,12 +82,18 @@ struct TreePlan {
   int32_t wide;        // many rows: the kernel that shares keys through LDS
   int32_t row_blocks;  // work-groups that the rows take
   int32_t padded;      // rows, to whole work-groups
-  int32_t splits;      // of the keys, by work-group
-  int32_t parts;       // of the keys at most (wide: two a split)
+  // Runs of keys: `groups` work-groups for each kv head and row block.
+  int32_t groups;
+  int32_t splits;      // runs of each sequence
+  int32_t balanced;    // or by the lengths on the device (wide), with
+  int32_t goal;        // runs to aim for,
+  int32_t least;       // tiles of a run at least
+  int32_t most_runs;   // and runs of a sequence at most
+  int32_t joined;      // a sequence may have several
   int32_t stored;      // accumulate: the scores pass through the workspace
   int64_t len_pad;     // max_len rounded up, of the stored scores
   // workspace offsets and total, bytes
-  size_t pO, pM, pL, row_m, row_inv, score, total;
+  size_t pO, pM, pL, share, row_m, row_inv, score, total;
 };
 
 struct TreeCall {
@@ -103,9 +109,10 @@ struct TreeCall {
   float scale_log2;          // of the logits, times log2(e)
   float decay;
   int32_t hq, n_tok, max_tree, max_len, accumulate;
-  float* pO;                 // [seq][kv head][part][row][d]
-  float* pM;                 // [seq][kv head][part][row] reference, log2 units
-  float* pL;                 //                            and sum
+  float* pO;                 // [part][kv head][row][d]
+  float* pM;                 // [part][kv head][row] reference, log2 units
+  float* pL;                 //                        and sum
+  int32_t* share;            // [seq] first part, parts
   float* row_m;              // [seq][kv head][row] the same, over the splits:
   float* row_inv;            // reference and 1 / sum (accumulate)
   float* score;              // [seq][kv head][row][len_pad + 64] q.k

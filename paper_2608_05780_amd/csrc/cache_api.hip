@@ -207,6 +207,7 @@ evisel_status evisel_tree_attention(
   t.pO = (float*)(w + p.pO);
   t.pM = (float*)(w + p.pM);
   t.pL = (float*)(w + p.pL);
+  t.share = (int32_t*)(w + p.share);
   t.row_m = (float*)(w + p.row_m);
   t.row_inv = (float*)(w + p.row_inv);
   t.score = (float*)(w + p.score);

@@ -12,7 +12,9 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kMaxTree = 64;
-constexpr int kMaxSplits = 128;
+constexpr int kMaxSplits = 128;   // parts that a row is joined from
+// Sequences up to which every work-group looks through all their lengths.
+constexpr int kMaxBalanced = 256;
 // Wavefronts of a work-group that takes 16 RT rows.
 constexpr int waves_of(int row_tiles) { return row_tiles == 4 ? 4 : 8; }
 
@@ -233,19 +235,93 @@ __device__ __forceinline__ Tree tree_of(const CacheView& c, const TreeCall& t,
   return r;
 }
 
-// Tiles of the cache and of the drafted tokens, and how many of them each of
-// `splits` parts takes.
-struct Parts {
-  int cached, total, per, used;
+// Tiles of kt keys: the cache's and the drafted tokens'; none without tokens.
+__device__ __forceinline__ int cached_tiles(const Tree& r, int kt) {
+  return (r.len + kt - 1) / kt;
+}
+__device__ __forceinline__ int tiles_of(const Tree& r, const TreeCall& t,
+                                        int kt) {
+  if (r.n == 0) return 0;
+  return max(1, cached_tiles(r, kt) + (t.k_new ? (r.n + kt - 1) / kt : 0));
+}
+
+// A work-group's run of keys: run `run` of the `used` ones of `per` tiles that
+// sequence `seq` has, whose parts start at index `slot`. seq is -1 if the
+// work-group has nothing to do. The first run of a sequence leaves slot and
+// used in the workspace for what joins the parts.
+struct Share {
+  int seq, run, per, used, slot;
 };
-__device__ __forceinline__ Parts parts_of(const Tree& r, bool drafts, int kt,
-                                          int splits) {
-  Parts p;
-  p.cached = (r.len + kt - 1) / kt;
-  p.total = p.cached + (drafts ? (r.n + kt - 1) / kt : 0);
-  p.per = max((p.total + splits - 1) / splits, 1);
-  p.used = max((p.total + p.per - 1) / p.per, 1);
-  return p;
+// The same number of runs for each sequence, whatever its length.
+__device__ __forceinline__ Share even_share(const CacheView& c,
+                                            const TreePlan& pl,
+                                            const TreeCall& t, int kt, int seq,
+                                            int run) {
+  Share r;
+  r.seq = seq;
+  r.run = run;
+  r.slot = seq * pl.splits;
+  const int n = tiles_of(tree_of(c, t, seq), t, kt);
+  r.per = max(1, (n + pl.splits - 1) / pl.splits);
+  r.used = (n + r.per - 1) / r.per;
+  if (run >= r.used) r.seq = -1;
+  return r;
+}
+// The tiles of all sequences over the work-groups that the card holds at
+// once, so that long and short sequences make work-groups of one size: every
+// wavefront finds its run for itself from the lengths on the device.
+__device__ __forceinline__ Share fair_share(const CacheView& c,
+                                            const TreePlan& pl,
+                                            const TreeCall& t, int kt,
+                                            int group) {
+  if (!pl.balanced)
+    return even_share(c, pl, t, kt, group / pl.splits, group % pl.splits);
+  Share r;
+  const int lane = threadIdx.x & 63;
+  auto tiles = [&](int s0) {
+    return s0 + lane < c.n_seq ? tiles_of(tree_of(c, t, s0 + lane), t, kt) : 0;
+  };
+  const int first = tiles(0), wide = min(c.n_seq, 64);
+  int total = 0, active = 0, longest = 0;
+  for (int s0 = 0; s0 < c.n_seq; s0 += 64) {
+    const int n = s0 ? tiles(s0) : first;
+    int sum = n, top = n;
+    for (int o = 1; o < wide; o <<= 1) {
+      sum += __shfl_xor(sum, o);
+      top = max(top, __shfl_xor(top, o));
+    }
+    total += __builtin_amdgcn_readfirstlane(sum);
+    longest = max(longest, __builtin_amdgcn_readfirstlane(top));
+    active += __popcll(__ballot(n > 0));
+  }
+  // a run left over at the end of each sequence fits in, too
+  const int room = max(pl.goal - active, (pl.goal + 1) / 2);
+  int per = (total + room - 1) / room;
+  per = max(max(per, pl.least), (longest + pl.most_runs - 1) / pl.most_runs);
+  r.per = __builtin_amdgcn_readfirstlane(per);
+  r.seq = -1;
+  r.run = r.used = r.slot = 0;
+  int before = 0;
+  for (int s0 = 0; s0 < c.n_seq; s0 += 64) {
+    const int n = s0 ? tiles(s0) : first, used = (n + r.per - 1) / r.per;
+    int run = used;
+    for (int o = 1; o < wide; o <<= 1) {
+      const int up = __shfl_up(run, o);
+      if (lane >= o) run += up;
+    }
+    run += before;   // of this sequence and all before it
+    const uint64_t here = __ballot(lane < wide && group < run);
+    if (here) {
+      const int l = __builtin_ctzll(here);
+      r.seq = s0 + l;
+      r.used = __builtin_amdgcn_readlane(used, l);
+      r.slot = __builtin_amdgcn_readlane(run, l) - r.used;
+      r.run = group - r.slot;
+      return r;
+    }
+    before = __builtin_amdgcn_readlane(run, wide - 1);
+  }
+  return r;
 }
 
 // Many rows (wide): a work-group takes 256 of them, kWideRows a wavefront,
@@ -258,15 +334,6 @@ constexpr int kWideKeys = 64;   // of a stage
 __device__ __forceinline__ int key_halves(int n_rows, int row0) {
   return n_rows - row0 <= kWideBlock / 2 ? 2 : 1;
 }
-// The parts that row r of a sequence is joined from.
-template <class P>
-__device__ __forceinline__ int row_parts(const TreePlan& pl, const Tree& tr,
-                                         bool drafts, int n_rows, int r) {
-  if (!pl.wide) return parts_of(tr, drafts, P::KT, pl.splits).used;
-  return parts_of(tr, drafts, kWideKeys, pl.splits).used *
-         key_halves(n_rows, r / kWideBlock * kWideBlock);
-}
-
 // Which drafted tokens token `lane` sees: itself and its ancestors. The lanes'
 // parents are followed by doubling, six times for 64 tokens.
 __device__ __forceinline__ uint64_t ancestors(const TreeCall& t, const Tree& r,
@@ -524,19 +591,27 @@ __global__ __launch_bounds__(64 * waves_of(RT), RT == 4 ? 1 : 2) void tree_kerne
   const int xcd = blockIdx.x % 8, y = blockIdx.x / 8;
   const int rb = y % pl.row_blocks;
   int unit = y / pl.row_blocks * 8 + xcd;
-  if (unit >= c.n_seq * c.hkv * pl.splits) return;
+  if (unit >= pl.groups * c.hkv) return;
   const int split = unit % pl.splits;
   unit /= pl.splits;
-  const int kvh = unit % c.hkv, seq = unit / c.hkv;
+  const int kvh = unit % c.hkv;
+  const Share sh = even_share(c, pl, t, KT, unit / c.hkv, split);
+  if (sh.seq < 0) return;
+  const int seq = sh.seq;
+  if (pl.joined && sh.run == 0 && kvh == 0 && rb == 0 && threadIdx.x == 0) {
+    t.share[2 * seq] = sh.slot;
+    t.share[2 * seq + 1] = sh.used;
+  }
+  unit = seq * c.hkv + kvh;
   const Tree tr = tree_of(c, t, seq);
   const int group = t.hq / c.hkv, n_rows = tr.n * group;
   const int row0 = rb * 16 * RT;
   if (row0 >= n_rows) return;
-  const Parts pt = parts_of(tr, t.k_new != nullptr, KT, pl.splits);
-  if (split >= pt.used) return;
   const int lane = threadIdx.x & 63, c16 = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int t0 = split * pt.per, t1 = min(t0 + pt.per, pt.total);
+  const int cached = cached_tiles(tr, KT);
+  const int t0 = sh.run * sh.per;
+  const int t1 = min(t0 + sh.per, tiles_of(tr, t, KT));
   const int64_t head = kvh * c.head_bytes;
   const uint32_t koff = (uint32_t)c16 * c.token_bytes + 16 * g;
   const uint32_t voff = (uint32_t)(4 * g) * c.token_bytes + c16 * P::kLaneV;
@@ -564,7 +639,7 @@ __global__ __launch_bounds__(64 * waves_of(RT), RT == 4 ? 1 : 2) void tree_kerne
                     : nullptr;
   }
 
-  const int c_end = min(t1, pt.cached);
+  const int c_end = min(t1, cached);
   int tile = t0 + wave;
   if (tile < c_end) {
     const int end = min(tr.len, c_end * KT);
@@ -616,9 +691,9 @@ __global__ __launch_bounds__(64 * waves_of(RT), RT == 4 ? 1 : 2) void tree_kerne
     take(No{});
   }
   for (tile = t0 + wave; tile < t1; tile += kWaves) {
-    if (tile < pt.cached) continue;
+    if (tile < cached || !t.k_new) continue;
     take_drafts<P, D, RT>(rows, c, t, tr, kvh, row0, n_rows,
-                          (tile - pt.cached) * KT,
+                          (tile - cached) * KT,
                           SCORE ? score[0] : nullptr, pl.len_pad, so[wave]);
   }
 
@@ -635,7 +710,7 @@ __global__ __launch_bounds__(64 * waves_of(RT), RT == 4 ? 1 : 2) void tree_kerne
   constexpr int kCols = 16 * D / (64 * kWaves);   // of a thread
   const int er = threadIdx.x / (D / kCols), ec = threadIdx.x % (D / kCols);
   const int padded = pl.padded;
-  const int64_t part = ((int64_t)unit * pl.parts + split) * padded;
+  const int64_t part = ((int64_t)(sh.slot + sh.run) * c.hkv + kvh) * padded;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     float top = neg_inf();
@@ -667,7 +742,7 @@ __global__ __launch_bounds__(64 * waves_of(RT), RT == 4 ? 1 : 2) void tree_kerne
 #pragma unroll
         for (int i = 0; i < kCols; ++i)
           x[i] += so[w][er * kPad + ec * kCols + i];
-      if (pt.used == 1) {
+      if (sh.used == 1) {
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
         for (int i = 0; i < kCols; ++i) x[i] *= inv;
@@ -719,17 +794,20 @@ __global__ __launch_bounds__(64 * kWideWaves, kWideRt == 2 ? 2 : 1) void tree_wi
   const int xcd = blockIdx.x % 8, y = blockIdx.x / 8;
   const int rb = y % pl.row_blocks;
   int unit = y / pl.row_blocks * 8 + xcd;
-  if (unit >= c.n_seq * c.hkv * pl.splits) return;
-  const int split = unit % pl.splits;
-  unit /= pl.splits;
-  const int kvh = unit % c.hkv, seq = unit / c.hkv;
+  if (unit >= pl.groups * c.hkv) return;
+  const int kvh = unit % c.hkv;
+  const Share sh = fair_share(c, pl, t, kWideKeys, unit / c.hkv);
+  if (sh.seq < 0) return;
+  const int seq = sh.seq;
+  if (pl.joined && sh.run == 0 && kvh == 0 && rb == 0 && threadIdx.x == 0) {
+    t.share[2 * seq] = sh.slot;
+    t.share[2 * seq + 1] = sh.used;
+  }
+  unit = seq * c.hkv + kvh;
   const Tree tr = tree_of(c, t, seq);
   const int group = t.hq / c.hkv, n_rows = tr.n * group;
   const int block0 = rb * kWideBlock;
   if (block0 >= n_rows) return;
-  const Parts pt =
-      parts_of(tr, t.k_new != nullptr, kWideKeys, pl.splits);
-  if (split >= pt.used) return;
   const int tid = threadIdx.x, lane = tid & 63, c16 = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int halves = key_halves(n_rows, block0);
@@ -759,7 +837,8 @@ __global__ __launch_bounds__(64 * kWideWaves, kWideRt == 2 ? 2 : 1) void tree_wi
     }
   }
 
-  const int s0 = split * pt.per, s1 = min(s0 + pt.per, pt.cached);
+  const int s0 = sh.run * sh.per;
+  const int s1 = min(s0 + sh.per, cached_tiles(tr, kWideKeys));
   auto k_swizzle = [](int r) { return RC == 16 ? r & 15 : (r >> 1) & 7; };
   // a transposing read names four keys, and of each four chunks, every
   // fourth (D = 64: every second, of two keys in a line of 256 bytes)
@@ -938,7 +1017,7 @@ __global__ __launch_bounds__(64 * kWideWaves, kWideRt == 2 ? 2 : 1) void tree_wi
   }
   rows.weigh(x, t);
   add_v(va, x);
-  if (t.k_new && split == pt.used - 1) {
+  if (t.k_new && sh.run == sh.used - 1) {
     // the drafted tokens, one stage; every row has keys of its own
     const int64_t token = (int64_t)c.hkv * (D * P::ES);
     const int64_t base = (int64_t)tr.first * token + kvh * (D * P::ES);
@@ -1023,9 +1102,9 @@ __global__ __launch_bounds__(64 * kWideWaves, kWideRt == 2 ? 2 : 1) void tree_wi
   if (!works) return;
 
   // every wavefront has its rows to itself: out, or its part of them
-  const int used = pt.used * halves;
+  const int used = sh.used * halves;
   const int64_t part =
-      ((int64_t)unit * pl.parts + split * halves + half) * pl.padded;
+      ((int64_t)(2 * (sh.slot + sh.run) + half) * c.hkv + kvh) * pl.padded;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const float sum = row_sum(rows.l[rt]), big = rows.m[rt];
@@ -1078,10 +1157,15 @@ __device__ __forceinline__ void join_row(const CacheView& c,
   const Tree tr = tree_of(c, t, seq);
   const int group = t.hq / c.hkv;
   if (r >= tr.n * group) return;
-  const int used =
-      row_parts<P>(pl, tr, t.k_new != nullptr, tr.n * group, r);
+  // A part of the row is `stride` behind the one before it. (wide: two a run,
+  // of which the second is used where the keys are halved)
+  const int halves =
+      pl.wide ? key_halves(tr.n * group, r / kWideBlock * kWideBlock) : 1;
+  const int slot = t.share[2 * seq], used = t.share[2 * seq + 1] * halves;
   if (used == 1) return;
-  const int64_t base = (int64_t)unit * pl.parts * padded + r;
+  const int64_t stride = (int64_t)c.hkv * padded * (pl.wide ? 3 - halves : 1);
+  const int64_t base =
+      ((int64_t)slot * (pl.wide ? 2 : 1) * c.hkv + kvh) * padded + r;
   const int lane = threadIdx.x & 63;
   // every wavefront finds the largest reference for itself
   float big = neg_inf();
@@ -1089,7 +1173,7 @@ __device__ __forceinline__ void join_row(const CacheView& c,
 #pragma unroll
   for (int u = 0; u < kMaxSplits / 64; ++u)
     if (lane + 64 * u < used)
-      big = fmaxf(big, t.pM[base + (int64_t)(lane + 64 * u) * padded]);
+      big = fmaxf(big, t.pM[base + (lane + 64 * u) * stride]);
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) big = fmaxf(big, __shfl_xor(big, o));
   const int e = 4 * (threadIdx.x % kLanes), gr = threadIdx.x / kLanes;
@@ -1097,7 +1181,7 @@ __device__ __forceinline__ void join_row(const CacheView& c,
   f32x4 x = {};
 #pragma unroll 4
   for (int s = gr; s < used; s += kGroups) {
-    const int64_t at = base + (int64_t)s * padded;
+    const int64_t at = base + s * stride;
     const float m = t.pM[at], l = t.pL[at];
     const f32x4 o = *(const f32x4*)(t.pO + at * D + e);
     const float f = m == neg_inf() ? 0.f : exp2_(m - big);
@@ -1159,7 +1243,8 @@ __global__ __launch_bounds__(kThreads) void mass_stored_kernel(
   const int64_t key0 = (int64_t)kb * kThreads * 4;
   if (tr.n == 0 || (key0 >= tr.len && kb > 0)) return;
   const int group = t.hq / c.hkv, n_rows = tr.n * group;
-  const Parts pt = parts_of(tr, t.k_new != nullptr, P::KT, pl.splits);
+  const int slot = pl.joined ? t.share[2 * seq] : 0;
+  const int used = pl.joined ? t.share[2 * seq + 1] : 1;
   const int tid = threadIdx.x;
   const int64_t key = key0 + 4 * tid;
   const int padded = pl.padded;
@@ -1168,16 +1253,17 @@ __global__ __launch_bounds__(kThreads) void mass_stored_kernel(
     const int r = tid / 16, l16 = tid % 16;
     float m = neg_inf(), cf = 0.f;
     if (r < n_rows) {
-      if (pt.used == 1) {
+      if (used == 1) {
         m = t.row_m[(int64_t)unit * padded + r];
         cf = t.row_inv[(int64_t)unit * padded + r];
       } else {
-        const int64_t base = (int64_t)unit * pl.parts * padded + r;
+        const int64_t stride = (int64_t)c.hkv * padded;
+        const int64_t base = ((int64_t)slot * c.hkv + kvh) * padded + r;
         float pm[kMaxSplits / 16], sum = 0.f;
 #pragma unroll
         for (int u = 0; u < kMaxSplits / 16; ++u) {
           const int s = l16 + 16 * u;
-          pm[u] = s < pt.used ? t.pM[base + (int64_t)s * padded] : neg_inf();
+          pm[u] = s < used ? t.pM[base + s * stride] : neg_inf();
           m = fmaxf(m, pm[u]);
         }
 #pragma unroll
@@ -1185,9 +1271,9 @@ __global__ __launch_bounds__(kThreads) void mass_stored_kernel(
 #pragma unroll
         for (int u = 0; u < kMaxSplits / 16; ++u) {
           const int s = l16 + 16 * u;
-          if (s < pt.used)
+          if (s < used)
             sum += (pm[u] == neg_inf() ? 0.f : exp2_(pm[u] - m)) *
-                   t.pL[base + (int64_t)s * padded];
+                   t.pL[base + s * stride];
         }
 #pragma unroll
         for (int o = 1; o < 16; o <<= 1) sum += __shfl_xor(sum, o);
@@ -1400,7 +1486,7 @@ __global__ __launch_bounds__(kThreads) void mass_kernel(const CacheView c,
 template <class P, int D>
 hipError_t launch_tree(const CacheView& c, const TreePlan& pl,
                        const TreeCall& t, hipStream_t s) {
-  const int64_t units = (int64_t)c.n_seq * c.hkv * pl.splits;
+  const int64_t units = (int64_t)pl.groups * c.hkv;
   const int64_t blocks = (units + 7) / 8 * 8 * pl.row_blocks;
   if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
   const dim3 grid((unsigned)blocks), block(kThreads);
@@ -1419,7 +1505,7 @@ hipError_t launch_tree(const CacheView& c, const TreePlan& pl,
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int64_t join =
-      pl.parts > 1 ? (int64_t)c.n_seq * c.hkv * pl.rows : 0;
+      pl.joined ? (int64_t)c.n_seq * c.hkv * pl.rows : 0;
   if (pl.stored) {
     const int kb = std::max(1, (t.max_len + 4 * kThreads - 1) / (4 * kThreads));
     const int64_t n = join + (int64_t)c.n_seq * c.hkv * kb;
@@ -1462,29 +1548,45 @@ TreePlan plan_tree(const CacheView& c, int32_t hq, int32_t max_tree,
       ((int64_t)max_len + kt - 1) / kt + (max_tree + kt - 1) / kt;
   const int64_t units = (int64_t)c.n_seq * c.hkv * p.row_blocks;
   int64_t splits = 1;
+  p.groups = c.n_seq;
   if (p.wide) {
-    // a work-group takes a CU: one round of them, four stages each at least
-    splits = std::max<int64_t>(1, 256 / units);
-    splits = std::min(splits, (tiles + 3) / 4);
-    splits = std::min<int64_t>(kMaxSplits / 2, splits);
+    // A work-group takes a CU, and four stages at least: one round of them
+    // (the row blocks of a run are on one XCD, which has 32 CUs). Even runs
+    // left CUs idle behind the longest of eight sequences of 1,100 to 16,512
+    // tokens: 70 us, 56 with fair ones.
+    p.least = 4;
+    p.most_runs = kMaxSplits / 2;
+    p.goal = (int32_t)std::max<int64_t>(
+        1, std::max(1, 32 / p.row_blocks) * 8 / c.hkv);
+    p.balanced = tiles > p.least && c.n_seq <= kMaxBalanced &&
+                 tiles * c.n_seq < 1 << 30;
+    if (p.balanced)
+      p.groups = p.goal + c.n_seq;
+    else
+      splits = std::min<int64_t>({256 / units, tiles / p.least, p.most_runs});
   } else {
     // Work-groups for the 256 CUs, as far as every wavefront gets a tile; more
     // of them, up to eight for each CU so that sequences of unlike lengths
     // even out, while each keeps 32 tiles. Up to five rounds of tiles a
     // work-group takes less than it and the second launch (one token over 544:
-    // 9.6 us, 10.2 with five splits). The 28 / 4 heads: 64 sequences of up to
-    // 8,000 tokens take 131 us with 8 splits, 138 with 4, 163 with one; eight
-    // with trees of 8 25 us with 8 splits, 31 with 16; 16 heads of their own,
-    // 16 sequences of up to 4,000: 61 us with 4 splits, 72 with 8, 73 with 1.
+    // 9.6 us, 10.2 with five splits; over 2,000: 22, 11.8 with eight). 28 / 4
+    // heads: 64 sequences of up to 8,000 tokens take 131 us with 8 splits, 138
+    // with 4, 163 with one; eight with trees of 8 25 us with 8 splits, 31 with
+    // 16; 16 heads of their own, 16 sequences of up to 4,000: 61 us with 4
+    // splits, 72 with 8, 73 with 1. Runs of one length for all sequences were
+    // slower here (64 of up to 8,000: 140), as their work-groups start and end
+    // together.
     const int w = waves_of(p.row_tiles);
     if (tiles > 5 * w) {
       splits = std::min<int64_t>(256 / units, (tiles + w - 1) / w);
-      splits = std::max(splits, std::min<int64_t>(2048 / units, (tiles + 31) / 32));
+      splits = std::max(splits,
+                        std::min<int64_t>(2048 / units, (tiles + 31) / 32));
       splits = std::min<int64_t>(kMaxSplits, splits);
     }
   }
   p.splits = (int32_t)std::max<int64_t>(1, splits);
-  p.parts = p.wide ? 2 * p.splits : p.splits;
+  if (!p.balanced) p.groups = c.n_seq * p.splits;
+  p.joined = p.wide || p.groups > c.n_seq;
   p.stored = accumulate && p.rows <= kStoredRows;
   p.len_pad = ((int64_t)max_len + 31) / 32 * 32;
   size_t off = 0;
@@ -1494,10 +1596,12 @@ TreePlan plan_tree(const CacheView& c, int32_t hq, int32_t max_tree,
     return at;
   };
   const size_t all = (size_t)c.n_seq * c.hkv * p.padded;   // rows
-  const size_t part = p.parts > 1 ? all * p.parts : 0;
+  const size_t part =
+      p.joined ? (size_t)p.groups * (p.wide ? 2 : 1) * c.hkv * p.padded : 0;
   p.pO = take(part * c.d * 4);
   p.pM = take(part * 4);
   p.pL = take(part * 4);
+  p.share = take(p.joined ? (size_t)c.n_seq * 8 : 0);
   p.row_m = take(accumulate ? all * 4 : 0);
   p.row_inv = take(accumulate ? all * 4 : 0);
   p.score = take(p.stored ? (size_t)c.n_seq * c.hkv * p.rows *
