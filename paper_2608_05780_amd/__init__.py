@@ -434,6 +434,15 @@ def _want(name, t, dtype, shape, dev):
     return t.data_ptr()
 
 
+def _stream_on(stream, dev):
+    """The stream's handle; by default torch's current one on device ``dev``
+    (by its handle alone: making torch's stream object takes 2.7 us)."""
+    if stream is None and dev >= 0:
+        import torch
+        return torch._C._cuda_getCurrentRawStream(dev)
+    return _stream(stream)
+
+
 class Cache:
     """One layer's key/value cache: a view of the caller's tensors, which it
     keeps alive. ``k`` and ``v`` are pages [n_pages, page, Hkv, d] (bf16 or
@@ -510,7 +519,7 @@ def cache_append(cache: Cache, k_new, v_new, tok_ptr, max_new: int,
         int(max_new),
         None if w_new is None else
         _want("w_new", w_new, torch.float32, (n, cache.hkv), dev),
-        _stream(stream))
+        _stream_on(stream, dev))
     if st:
         _check(st)
 
@@ -565,7 +574,7 @@ def tree_attention(cache: Cache, q, k_new, v_new, tree_ptr, out, workspace,
         0.0 if decay is None else decay,
         None if w_new is None else
         _want("w_new", w_new, f32, (n, cache.hkv), dev),
-        *_scratch(workspace, dev), _stream(stream))
+        *_scratch(workspace, dev), _stream_on(stream, dev))
     if st:
         _check(st)
 
@@ -594,7 +603,7 @@ def cache_evict(cache: Cache, budget: int, workspace, n_sink: int = 0,
     st = (_lib or load()).evisel_cache_evict(
         cache._ref, int(budget), int(n_sink), int(n_recent),
         cache.capacity if max_len is None else int(max_len),
-        *_scratch(workspace, dev), _stream(stream))
+        *_scratch(workspace, dev), _stream_on(stream, dev))
     if st:
         _check(st)
 

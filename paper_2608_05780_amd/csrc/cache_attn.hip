@@ -164,15 +164,18 @@ struct TreeF32 {
 #pragma unroll
     for (int j = 0; j < KS; ++j) r.x[j] = f32x4{};
   }
+  // Four sums, which are added at the end: a quarter of the roundings at the
+  // size of the whole logit (one sum: 1.6e-6 of the output at d = 64, plain
+  // fp32 4.5e-7).
   static __device__ f32x4 qk(const Row& k, const Row& q) {
-    f32x4 s = {};
+    f32x4 s[4] = {};
 #pragma unroll
     for (int j = 0; j < KS; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        s = __builtin_amdgcn_mfma_f32_16x16x4f32(k.x[j][e], q.x[j][e], s, 0, 0,
-                                                 0);
-    return s;
+        s[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(k.x[j][e], q.x[j][e], s[e],
+                                                    0, 0, 0);
+    return (s[0] + s[1]) + (s[2] + s[3]);
   }
   typedef Val ValT;   // one key a step: as it came
   static __device__ void turn(ValT& o, const Val& v) { o = v; }
@@ -1323,16 +1326,13 @@ __global__ __launch_bounds__(kThreads) void mass_stored_kernel(
 
 // Many rows: the logits are formed again, 16 NK keys a wavefront, whose rows
 // stay in registers while the query rows pass by in LDS, 128 at a time.
-template <class P>
-constexpr int kMassHalves = P::ES == 2 ? 4 : 2;
+constexpr int kMassHalves = 2;
 constexpr int kMassRows = 128;
 
 template <class P, int D>
-__global__ __launch_bounds__(kThreads) void mass_kernel(const CacheView c,
-                                                        const TreePlan pl,
-                                                        const TreeCall t,
-                                                        int key_blocks) {
-  constexpr int NK = kMassHalves<P>, TK = 16 * NK;
+__global__ __launch_bounds__(kThreads, P::ES == 2 ? 4 : 2) void mass_kernel(
+    const CacheView c, const TreePlan pl, const TreeCall t, int key_blocks) {
+  constexpr int NK = kMassHalves, TK = 16 * NK;
   constexpr int RC = D * P::ES / 16;   // 16-byte chunks of a row
   __shared__ __attribute__((aligned(16))) char qs[kMassRows * D * P::ES];
   __shared__ float ref[kMassRows], coef[kMassRows];
@@ -1521,7 +1521,7 @@ hipError_t launch_tree(const CacheView& c, const TreePlan& pl,
     if (e != hipSuccess) return e;
   }
   if (t.accumulate) {
-    constexpr int TK = 16 * kMassHalves<P>;
+    constexpr int TK = 16 * kMassHalves;
     const int tiles = (t.max_len + TK - 1) / TK + (t.max_tree + TK - 1) / TK;
     const int kb = (tiles + kThreads / 64 - 1) / (kThreads / 64);
     const int64_t n = (int64_t)c.n_seq * c.hkv * kb;
