@@ -371,6 +371,7 @@ evisel_status evisel_frame_evidence(const evisel_mask* mask,
  *   pos         device int32 [n_seq][hkv][capacity] (evict; append when
  *               given)
  * Every layer has its own view with its own length, seen, weight and pos.
+ * No buffer that a call writes may overlap another one of the call.
  * Requires n_seq >= 1, hkv >= 1, d = 64 or 128, page a power of two from 16
  * to 2^20, a capacity of at most 2^30 slots, strides of at least d and at
  * most 2^24 elements (page_stride: any) that keep the rows apart. */

@@ -437,7 +437,9 @@ def _want(name, t, dtype, shape, dev):
 def _stream_on(stream, dev):
     """The stream's handle; by default torch's current one on device ``dev``
     (by its handle alone: making torch's stream object takes 2.7 us)."""
-    if stream is None and dev >= 0:
+    if dev < 0:
+        raise ValueError("the cache is in host memory")
+    if stream is None:
         import torch
         return torch._C._cuda_getCurrentRawStream(dev)
     return _stream(stream)
@@ -489,8 +491,7 @@ class Cache:
         self._ref = ctypes.byref(self._view)
 
     def _checks(self):
-        """The device of a call's tensors: the cache's, which must be current
-        (a cache in host memory passes: the library refuses what it must)."""
+        """The device of a call's tensors: the cache's, which must be current."""
         if self.device_index >= 0:
             import torch
             if torch.cuda.current_device() != self.device_index:

@@ -68,8 +68,8 @@ __device__ __forceinline__ void append_tokens(const CacheView& c,
   if (!c.weight && !c.pos) return;
   // heads slowest: the slots of one head are neighbours
   const int n = i1 - i0;
-  for (int64_t u = tid; u < (int64_t)n * c.hkv; u += THREADS) {
-    const int h = (int)(u / n), i = i0 + (int)(u % n);
+  for (int u = tid; u < n * c.hkv; u += THREADS) {
+    const int h = u / n, i = i0 + u % n;
     const int64_t at = ((int64_t)seq * c.hkv + h) * c.cap + r.len + i;
     if (c.pos) c.pos[at] = r.seen + i;
     if (c.weight) {

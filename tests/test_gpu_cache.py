@@ -370,7 +370,7 @@ def test_evict_long():
     run_evict(t, 9000, 4, 1000)
 
 
-@pytest.mark.parametrize("n", [300, 37000])
+@pytest.mark.parametrize("n", [300, 9001, 37000])
 @pytest.mark.parametrize("what", ["equal", "zeros", "two", "odd", "tiny"])
 def test_evict_ranks(what, n):
     """Ties to the lowest slot; NaN like -inf, -0 like 0, infinities,
@@ -461,6 +461,92 @@ def test_results_do_not_depend_on_the_run():
         b = attend(t, x, decay=0.5)
         for k in a:
             assert np.array_equal(a[k], b[k]), k
+
+
+@pytest.mark.parametrize("n_seq", [70, 300])
+def test_many_sequences(n_seq):
+    """More sequences than lanes, and than those whose lengths every work-group
+    looks through; idle ones among them."""
+    import torch
+    rng = np.random.default_rng(n_seq)
+    lens = tuple(int(x) for x in rng.integers(0, 200, n_seq))
+    lens = lens[:-2] + (700, 0)
+    ns = [int(x) for x in rng.integers(0, 6, n_seq)]
+    ns[3], ns[-1] = 14, 3
+    say(f"  {n_seq} sequences")
+    t, r = H.make(torch, lens, 1, 64, "bf16", page=32)
+    x = H.tokens(torch, r, ns, 6, 1, 64, "bf16")
+    check(t, x, "bf16", decay=0.5)
+    x = H.tokens(torch, r, [min(n, 1) for n in ns], 6, 1, 64, "bf16")
+    check(t, x, "bf16", decay=0.5)
+    run_append(t, x["k_new"], x["v_new"], x["tree_ptr"], 1)
+    run_evict(t, 60, 4, 8)
+
+
+def test_long_runs_and_row_blocks():
+    """Many rows over a long cache next to a short one: several runs, two
+    blocks of rows, the second one's keys halved."""
+    import torch
+    t, rng = H.make(torch, (6000, 90, 0), 1, 128, "bf16", page=64)
+    x = H.tokens(torch, rng, [50, 9, 64], 7, 1, 128, "bf16")
+    check(t, x, "bf16", decay=1.0)
+    t["page_table"][0, 40] = -1
+    t["page_table"][0, 93] = 1 << 20
+    check(t, x, "bf16")
+
+
+def test_two_calls_at_once():
+    """Two caches on two streams with workspaces of their own: what each call
+    gives alone."""
+    import torch
+    both = []
+    for seed in (1, 2):
+        t, rng = H.make(torch, (3000, 400), 2, 128, "bf16", page=64, seed=seed)
+        x = H.tokens(torch, rng, [20, 3], 14, 2, 128, "bf16")
+        w0 = t["weight"].clone()
+        alone = attend(t, x, decay=1.0)
+        t["weight"].copy_(w0)
+        both.append((t, x, alone, torch.cuda.Stream()))
+    ev = pytest.ev
+    outs = []
+    torch.cuda.synchronize()
+    for t, x, _, s in both:
+        c = H.cache_of(ev, t)
+        with torch.cuda.stream(s):
+            out = torch.empty_like(x["q"])
+            lse = torch.empty(14, x["q"].shape[0], device="cuda")
+            ws = torch.empty(ev.tree_attention_workspace(
+                c, 14, 20, c.capacity, True), dtype=torch.uint8, device="cuda")
+            ev.tree_attention(c, x["q"], x["k_new"], x["v_new"],
+                              x["tree_ptr"], out, ws, 20, c.capacity,
+                              parent=x["parent"], lse=lse, decay=1.0)
+            outs.append((out, lse, ws))
+    torch.cuda.synchronize()
+    for (t, _, alone, _), (out, lse, _) in zip(both, outs):
+        got = H.host({"out": out, "lse": lse, "weight": t["weight"]})
+        for k in got:
+            assert np.array_equal(got[k], alone[k]), k
+
+
+def test_host_memory_is_refused():
+    import torch
+    ev = pytest.ev
+    t, rng = H.make(torch, (5,), 1, 64, "bf16", device="cpu")
+    x = H.tokens(torch, rng, [1], 2, 1, 64, "bf16", device="cpu")
+    c = H.cache_of(ev, t)
+    ws = torch.empty(1 << 16, dtype=torch.uint8)
+    with pytest.raises(ValueError):
+        ev.tree_attention(c, x["q"], x["k_new"], x["v_new"], x["tree_ptr"],
+                          torch.empty_like(x["q"]), ws, 1, 5)
+    with pytest.raises(ValueError):
+        ev.cache_append(c, x["k_new"], x["v_new"], x["tree_ptr"], 1)
+    with pytest.raises(ValueError):
+        ev.cache_evict(c, 2, ws)
+    # and tensors of the other place than the cache's
+    d = {k: v.cuda() for k, v in t.items()}
+    with pytest.raises(ValueError):
+        ev.cache_append(H.cache_of(ev, d), x["k_new"], x["v_new"],
+                        x["tree_ptr"].cuda(), 1)
 
 
 def test_other_stream():
