@@ -449,6 +449,58 @@ def test_generation_together():
     assert int(t["length"].max()) == 96
 
 
+def test_after_the_probe():
+    """The probe's own path and on from it: a prefilled video (all-causal
+    rule) enters the cache with its evidence as first weights, and its last
+    query token, attended over the cache, gets what the prefill gave it; then
+    the cache is cut by those weights and the frames that held the evidence
+    are still there."""
+    import torch
+    ev = pytest.ev
+    frames, text, nv, hq, hkv, d = 20, 9, 16, 8, 2, 128
+    S = frames * nv + text
+    g = torch.Generator(device="cuda").manual_seed(3)
+    rnd = lambda *s: torch.randn(*s, generator=g, device="cuda")
+    q, k, v = rnd(S, hq, d), rnd(S, hkv, d), rnd(S, hkv, d)
+    # the query tokens look at frames 6 and 13
+    way = rnd(hkv, d)
+    for f in (6, 13):
+        k[f * nv:(f + 1) * nv] += 0.7 * way
+    q[frames * nv:] += 0.7 * way.repeat_interleave(hq // hkv, 0)
+    q, k, v = (x.to(torch.bfloat16) for x in (q, k, v))
+    mask = ev.build_block_mask([frames], [text], nv, 64, 1, -1, hq, hkv)
+    out = torch.empty_like(q)
+    lse = torch.empty(hq, S, device="cuda")
+    evid = torch.empty(1, hq, frames, device="cuda")
+    ws = torch.empty(ev.sparse_prefill_workspace(mask, d), dtype=torch.uint8,
+                     device="cuda")
+    ev.sparse_prefill(mask, 0, 1, q, k, v, out, evid, ws, lse=lse)
+    t, _ = H.make(torch, (0,), hkv, d, "bf16", page=16, extra=S)
+    w0 = torch.zeros(S, hkv, device="cuda")
+    per_kv = evid[0].view(hkv, hq // hkv, frames).sum(1) / nv
+    w0[:frames * nv] = per_kv.t().repeat_interleave(nv, 0)
+    ptr = torch.tensor([0, S - 1], dtype=torch.int32, device="cuda")
+    run_append(t, k, v, ptr, S, w_new=w0)
+    x = {"q": q[-1:].contiguous(), "k_new": k[-1:].contiguous(),
+         "v_new": v[-1:].contiguous(),
+         "tree_ptr": torch.tensor([0, 1], dtype=torch.int32, device="cuda"),
+         "parent": torch.tensor([-1], dtype=torch.int32, device="cuda")}
+    got = check(t, x, "bf16", decay=1.0)
+    # both round the probabilities and the output to bf16
+    h = H.host({"out": out[-1:], "lse": lse[:, -1:]})
+    ref = oc.tree_attention(H.host(t), *(H.host(x)[n] for n in (
+        "q", "k_new", "v_new", "tree_ptr", "parent")), d ** -0.5)
+    bound = 2 * 2.0 ** -8 * (ref["absv"] + np.abs(ref["out"])) * 1.01
+    assert (np.abs(h["out"] - got["out"]) <= bound).all()
+    assert np.abs(h["lse"] - got["lse"]).max() <= 1e-5
+    run_evict(t, 64, 2, 9)
+    pos = t["pos"][0, :, :64].cpu().numpy()
+    for g in range(hkv):
+        kept = set(pos[g].tolist())
+        for f in (6, 13):
+            assert kept >= set(range(f * nv, (f + 1) * nv))
+
+
 def test_results_do_not_depend_on_the_run():
     """The same call again, with another workspace: the same bits."""
     import torch
