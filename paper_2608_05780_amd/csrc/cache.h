@@ -66,7 +66,15 @@ struct EvictCall {
   int32_t* count;      // [n_seq][hkv] moves
   int32_t* from;       // [n_seq][hkv][max_moves] slots
   int32_t* to;
+  // long caches (null otherwise): what a slot ranks by [n_seq][hkv][key_stride]
+  // and histograms [n_seq][hkv][chunks][2048]
+  uint32_t* keys;
+  uint32_t* chunk_hist;
+  int32_t chunks, key_stride;
 };
+// Sets max_moves and the workspace pointers from budget and max_len; the
+// workspace's bytes.
+size_t evict_layout(const CacheView& c, EvictCall& e, char* workspace);
 hipError_t launch_cache_evict(const CacheView& c, const EvictCall& e,
                               hipStream_t s);
 

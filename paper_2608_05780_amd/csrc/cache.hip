@@ -175,13 +175,13 @@ __device__ __forceinline__ uint32_t below4(int i, int end) {
 constexpr int kEvThreads = 1024;
 constexpr int kEvWaves = kEvThreads / 64;
 constexpr int kEvBins = 2048;
+// Keys that stay in LDS (the select kernel's other arrays take 65 KB of 160).
+constexpr int kEvLdsKeys = 23 * 1024;
 // Histograms side by side, lane by lane: equal weights are 16 additions to one
 // place and not 64, and the four neighbours lie in different banks.
 constexpr int kEvCopies = 4;
 // keys of one digit's bin that are kept as a list, with their slots
 constexpr int kEvList = 4096;
-// keys that stay in LDS (the kernel's other arrays take 65 KB of the 160)
-constexpr int kEvLdsKeys = 23 * 1024;
 
 // Sum over the lanes before this one, and over all (wave-uniform).
 __device__ __forceinline__ uint32_t lanes_before(uint32_t x, int lane,
@@ -196,6 +196,60 @@ __device__ __forceinline__ uint32_t lanes_before(uint32_t x, int lane,
   return run - x;
 }
 
+// Keys of a long cache, and the histogram of their first digit, kEvChunk slots
+// a work-group: what one work-group does alone in 16 us for 65,664 slots, with
+// the same again in both passes that follow (44 us in all, 37 so).
+constexpr int kEvChunk = 4096;
+constexpr int kKeyThreads = 256;
+__global__ __launch_bounds__(kKeyThreads) void evict_keys_kernel(
+    const CacheView c, const EvictCall e) {
+  __shared__ uint32_t hist[kEvBins * kEvCopies];
+  const int unit = blockIdx.x / e.chunks, chunk = blockIdx.x % e.chunks;
+  const int seq = unit / c.hkv, tid = threadIdx.x;
+  const int len = held(c, seq, e.max_len);
+  const int i0 = chunk * kEvChunk, i1 = min(i0 + kEvChunk, len);
+  if (len <= e.budget || i0 >= len) return;
+  const uint32_t span = (uint32_t)max(
+      (int64_t)0, (int64_t)c.seen[seq] - e.n_recent - e.n_sink);
+  const float* w = c.weight + (int64_t)unit * c.cap;
+  const int32_t* pos = c.pos + (int64_t)unit * c.cap;
+  uint32_t* keys = e.keys + (int64_t)unit * e.key_stride;
+  for (int i = 4 * tid; i < kEvBins * kEvCopies; i += 4 * kKeyThreads)
+    *(u32x4*)(hist + i) = u32x4{};
+  __syncthreads();
+  constexpr int kSteps = kEvChunk / (4 * kKeyThreads);
+  f32x4 x[kSteps];
+  i32x4 p[kSteps];
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s) {
+    const int i = i0 + 4 * (tid + s * kKeyThreads);
+    if (i < i1) {   // (the capacity is a multiple of 16)
+      x[s] = *(const f32x4*)(w + i);
+      p[s] = *(const i32x4*)(pos + i);
+    }
+  }
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s) {
+    const int i = i0 + 4 * (tid + s * kKeyThreads);
+    if (i >= i1) continue;
+    u32x4 k;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      k[u] = keep_key(x[s][u], p[s][u], e.n_sink, span);
+      if (i + u < i1)
+        atomicAdd(&hist[(k[u] >> 21) * kEvCopies + tid % kEvCopies], 1u);
+    }
+    *(u32x4*)(keys + i) = k;
+  }
+  __syncthreads();
+  uint32_t* out =
+      e.chunk_hist + ((int64_t)unit * e.chunks + chunk) * kEvBins;
+  for (int i = tid; i < kEvBins; i += kKeyThreads) {
+    const u32x4 h = *(const u32x4*)(hist + 4 * i);
+    out[i] = h[0] + h[1] + h[2] + h[3];
+  }
+}
+
 // One work-group per sequence and kv head: which slots it keeps, and from
 // that the moves. The budget-th largest key comes digit by digit, 11, 11 and
 // 10 bits, a histogram each. The first takes every key; a second pass, in
@@ -204,8 +258,8 @@ __device__ __forceinline__ uint32_t lanes_before(uint32_t x, int lane,
 // list (on all keys, if they are too many). Equal keys are kept from the
 // lowest slot on. The third pass knows how many holes and kept tail slots the
 // runs before hold and writes its own into the two lists, 256 slots at a time.
-// LDS: the keys stay there between the passes; otherwise each pass makes them
-// again from weight and pos.
+// LDS: the keys stay there between the passes. Otherwise evict_keys_kernel has
+// left them in the workspace, with the first digit's histograms by chunk.
 template <bool LDS>
 __global__ __launch_bounds__(kEvThreads) void evict_select_kernel(
     const CacheView c, const EvictCall e) {
@@ -241,9 +295,9 @@ __global__ __launch_bounds__(kEvThreads) void evict_select_kernel(
       k[u] = keep_key(x[u], p[u], e.n_sink, span);
     return k;
   };
-  auto four = [&](int i) {
-    return LDS ? *(const u32x4*)(keys + i) : make(i);
-  };
+  const uint32_t* made =
+      LDS ? nullptr : e.keys + (int64_t)unit * e.key_stride;
+  auto four = [&](int i) { return *(const u32x4*)((LDS ? keys : made) + i); };
   auto count = [&](uint32_t bin) {
     atomicAdd(&hist[bin * kEvCopies + lane % kEvCopies], 1u);
   };
@@ -286,17 +340,31 @@ __global__ __launch_bounds__(kEvThreads) void evict_select_kernel(
   if (tid == 0) listed = 0;
   if (tid < 4 * kEvWaves) runs[tid / kEvWaves][tid % kEvWaves] = 0;
   clear();
+  if (LDS) {
 #pragma unroll 2
-  for (int i = 4 * tid; i < len; i += kStep) {
-    const u32x4 k = make(i);
-    if (LDS) *(u32x4*)(keys + i) = k;
-    if (i + 4 <= len) {
+    for (int i = 4 * tid; i < len; i += kStep) {
+      const u32x4 k = make(i);
+      *(u32x4*)(keys + i) = k;
+      if (i + 4 <= len) {
 #pragma unroll
-      for (int u = 0; u < 4; ++u) count(k[u] >> 21);
-    } else {
-      for (int u = 0; u < (len & 3); ++u)
-        count((u == 0 ? k[0] : u == 1 ? k[1] : k[2]) >> 21);
+        for (int u = 0; u < 4; ++u) count(k[u] >> 21);
+      } else {
+        for (int u = 0; u < (len & 3); ++u)
+          count((u == 0 ? k[0] : u == 1 ? k[1] : k[2]) >> 21);
+      }
     }
+  } else {
+    const uint32_t* part = e.chunk_hist + (int64_t)unit * e.chunks * kEvBins;
+    const int n = (len + kEvChunk - 1) / kEvChunk;
+    uint32_t s[2] = {};
+#pragma unroll 8
+    for (int i = 0; i < n; ++i)
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        s[u] += part[(int64_t)i * kEvBins + tid + u * kEvThreads];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+      hist[(tid + u * kEvThreads) * kEvCopies] = s[u];
   }
   uint32_t need = (uint32_t)e.budget;   // keys still wanted among the matching
   locate(need);
@@ -307,11 +375,26 @@ __global__ __launch_bounds__(kEvThreads) void evict_select_kernel(
   // the keys that have it
   const int per = ((len + 256 * kEvWaves - 1) / (256 * kEvWaves)) * 256;
   const int a = min(wave * per, len), b = min(a + per, len);
+  // f(keys i .. i + 3, i) over the wavefront's run, 256 slots at a time, all
+  // lanes together (zeros past its end); kAhead of them are on their way
+  auto run = [&](auto f) {
+    constexpr int kAhead = LDS ? 2 : 8;
+    for (int i0 = a; i0 < b; i0 += 256 * kAhead) {
+      u32x4 k[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int i = i0 + 256 * u + 4 * lane;
+        k[u] = u32x4{};
+        if (i < b) k[u] = four(i);
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        if (i0 + 256 * u < b) f(k[u], i0 + 256 * u + 4 * lane);
+    }
+  };
   {
     int lo = 0, hi = 0;   // keys above, by side of the budget
-#pragma unroll 2
-    for (int i = a + 4 * lane; i < b; i += 256) {
-      const u32x4 k = four(i);
+    run([&](const u32x4& k, int i) {
       uint32_t gt = 0, eq = 0;
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
@@ -331,7 +414,7 @@ __global__ __launch_bounds__(kEvThreads) void evict_select_kernel(
           list_slot[at] = i + u;
         }
       }
-    }
+    });
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
       lo += __shfl_xor(lo, o);
@@ -397,11 +480,7 @@ __global__ __launch_bounds__(kEvThreads) void evict_select_kernel(
   int32_t* to = e.to + (int64_t)unit * e.max_moves;
   int32_t* from = e.from + (int64_t)unit * e.max_moves;
   const bool ties = all_eq > (int)need;   // some equal keys go
-#pragma unroll 2
-  for (int i0 = a; i0 < b; i0 += 256) {
-    const int i = i0 + 4 * lane;
-    u32x4 k = {};
-    if (i < b) k = four(i);
+  run([&](const u32x4& k, int i) {
     // slots in order: lane by lane, each its four
     uint32_t keep = 0, same = 0;
 #pragma unroll
@@ -429,7 +508,7 @@ __global__ __launch_bounds__(kEvThreads) void evict_select_kernel(
     for (; tail; tail &= tail - 1) from[s++] = i + __builtin_ctz(tail);
     holes += (int)(all & 0xFFFFu);
     tails += (int)(all >> 16);
-  }
+  });
   if (wave == kEvWaves - 1 && lane == 0) e.count[unit] = tails;
 }
 
@@ -519,11 +598,33 @@ hipError_t launch_cache_append(const CacheView& c, const AppendCall& a,
   return launch_append<32>(c, a, s);
 }
 
+size_t evict_layout(const CacheView& c, EvictCall& e, char* w) {
+  const size_t n = (size_t)c.n_seq * c.hkv;
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    char* const at = w + off;
+    off += (bytes + 255) & ~size_t(255);
+    return at;
+  };
+  e.max_moves = std::max(0, std::min(e.budget, e.max_len - e.budget));
+  e.count = (int32_t*)take(n * 4);
+  e.from = (int32_t*)take(n * e.max_moves * 4);
+  e.to = (int32_t*)take(n * e.max_moves * 4);
+  e.keys = e.chunk_hist = nullptr;
+  if (e.max_len > kEvLdsKeys && e.max_moves) {
+    e.chunks = (e.max_len + kEvChunk - 1) / kEvChunk;
+    e.key_stride = (e.max_len + 3) & ~3;
+    e.keys = (uint32_t*)take(n * e.key_stride * 4);
+    e.chunk_hist = (uint32_t*)take(n * e.chunks * kEvBins * 4);
+  }
+  return off;
+}
+
 hipError_t launch_cache_evict(const CacheView& c, const EvictCall& e,
                               hipStream_t s) {
   const dim3 grid((unsigned)(c.n_seq * c.hkv)), block(kEvThreads);
   if ((int64_t)c.n_seq * c.hkv > 0x7FFFFFFF) return hipErrorInvalidValue;
-  if (e.max_len <= kEvLdsKeys) {
+  if (!e.keys) {
     const size_t lds = ((size_t)e.max_len * 4 + 15) & ~size_t(15);
     if (lds > 0) {   // with the static arrays past 64 KB
       const hipError_t r = hipFuncSetAttribute(
@@ -533,6 +634,11 @@ hipError_t launch_cache_evict(const CacheView& c, const EvictCall& e,
     }
     evict_select_kernel<true><<<grid, block, lds, s>>>(c, e);
   } else {
+    const int64_t n = (int64_t)c.n_seq * c.hkv * e.chunks;
+    if (n > 0x7FFFFFFF) return hipErrorInvalidValue;
+    evict_keys_kernel<<<dim3((unsigned)n), dim3(kKeyThreads), 0, s>>>(c, e);
+    const hipError_t r = hipGetLastError();
+    if (r != hipSuccess) return r;
     evict_select_kernel<false><<<grid, block, 0, s>>>(c, e);
   }
   const hipError_t r = hipGetLastError();

@@ -77,17 +77,6 @@ evisel_status check_cache(const evisel_cache* c, evisel::CacheView* out) {
   return EVISEL_OK;
 }
 
-size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
-
-// Workspace of an eviction: counts, then the two slot lists.
-size_t evict_layout(const evisel::CacheView& c, int32_t budget,
-                    int32_t max_len, evisel::EvictCall* e) {
-  const size_t n = (size_t)c.n_seq * c.hkv;
-  e->max_moves = std::max(0, std::min(budget, max_len - budget));
-  const size_t lists = align256(n * e->max_moves * 4);
-  return align256(n * 4) + 2 * lists;
-}
-
 // Query heads of a kv head (the kernels' division by it is exact up to 2^13).
 constexpr int kMaxGroup = 4096;
 
@@ -224,7 +213,9 @@ size_t evisel_cache_evict_workspace(const evisel_cache* cache, int32_t budget,
   if (check_cache(cache, &c) != EVISEL_OK || budget < 1 || max_len < 0 ||
       max_len > c.cap)
     return 0;
-  return evict_layout(c, budget, max_len, &e);
+  e.budget = budget;
+  e.max_len = max_len;
+  return evisel::evict_layout(c, e, nullptr);
 }
 
 evisel_status evisel_cache_evict(const evisel_cache* cache, int32_t budget,
@@ -242,7 +233,11 @@ evisel_status evisel_cache_evict(const evisel_cache* cache, int32_t budget,
   if (max_len < 0 || max_len > c.cap)
     return bad("need 0 <= max_len <= capacity");
   evisel::EvictCall e;
-  const size_t need = evict_layout(c, budget, max_len, &e);
+  e.budget = budget;
+  e.n_sink = n_sink;
+  e.n_recent = n_recent;
+  e.max_len = max_len;
+  const size_t need = evisel::evict_layout(c, e, (char*)workspace);
   if (e.max_moves == 0) return EVISEL_OK;   // no sequence is over the budget
   if (!workspace || workspace_bytes < need)
     return set_error(EVISEL_ERR_WORKSPACE,
@@ -250,15 +245,6 @@ evisel_status evisel_cache_evict(const evisel_cache* cache, int32_t budget,
   if (!aligned(workspace, 256))
     return set_error(EVISEL_ERR_WORKSPACE,
                      "workspace must be 256-byte aligned");
-  e.budget = budget;
-  e.n_sink = n_sink;
-  e.n_recent = n_recent;
-  e.max_len = max_len;
-  const size_t n = (size_t)c.n_seq * c.hkv;
-  char* w = (char*)workspace;
-  e.count = (int32_t*)w;
-  e.from = (int32_t*)(w + align256(n * 4));
-  e.to = (int32_t*)(w + align256(n * 4) + align256(n * e.max_moves * 4));
   const hipError_t err =
       evisel::launch_cache_evict(c, e, (hipStream_t)stream);
   if (err != hipSuccess) return evisel::set_hip_error(err, "cache evict launch");
