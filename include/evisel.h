@@ -457,7 +457,8 @@ evisel_status evisel_tree_attention(
     const float* vote, float decay, float* w_new, void* workspace,
     size_t workspace_bytes, void* stream);
 
-/* Bytes of workspace of such a call (0 for arguments that it refuses). */
+/* Bytes of workspace of such a call (0 for arguments that it refuses, or if it
+ * needs none). */
 size_t evisel_tree_attention_workspace(const evisel_cache* cache, int32_t hq,
                                        int32_t max_tree, int32_t max_len,
                                        int32_t accumulate);

@@ -1597,8 +1597,13 @@ TreePlan plan_tree(const CacheView& c, int32_t hq, int32_t max_tree,
   p.splits = (int32_t)std::max<int64_t>(1, splits);
   if (!p.balanced) p.groups = c.n_seq * p.splits;
   p.joined = p.wide || p.groups > c.n_seq;
-  p.stored = accumulate && p.rows <= kStoredRows;
+  // Few rows' logits pass through the workspace (one token of 28 / 4 heads: 56
+  // bytes a key there and back, 256 for K again), unless a loose bound on the
+  // lengths would make that more than 1 GiB.
   p.len_pad = ((int64_t)max_len + 31) / 32 * 32;
+  const size_t scores = (size_t)c.n_seq * c.hkv * p.rows *
+                        (p.len_pad + kMaxTree) * 4;
+  p.stored = accumulate && p.rows <= kStoredRows && scores <= size_t(1) << 30;
   size_t off = 0;
   auto take = [&](size_t bytes) {
     const size_t at = off;
@@ -1614,9 +1619,7 @@ TreePlan plan_tree(const CacheView& c, int32_t hq, int32_t max_tree,
   p.share = take(p.joined ? (size_t)c.n_seq * 8 : 0);
   p.row_m = take(accumulate ? all * 4 : 0);
   p.row_inv = take(accumulate ? all * 4 : 0);
-  p.score = take(p.stored ? (size_t)c.n_seq * c.hkv * p.rows *
-                                (p.len_pad + kMaxTree) * 4
-                          : 0);
+  p.score = take(p.stored ? scores : 0);
   p.total = off;
   return p;
 }

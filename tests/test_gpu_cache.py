@@ -246,6 +246,26 @@ def test_more_splits_than_work_and_fewer():
     check(t, x, "bf16")
 
 
+def test_loose_bound():
+    """A bound of 2^25 tokens on a cache of 300: the workspace stays within 1
+    GiB for the logits of 16 rows, and the weights are the same."""
+    import torch
+    ev = pytest.ev
+    t, rng = H.make(torch, (300,), 1, 64, "bf16", page=64)
+    cap = 1 << 25
+    table = torch.full((1, cap // 64), -1, dtype=torch.int32, device="cuda")
+    table[:, :t["page_table"].shape[1]] = t["page_table"]
+    old = t["weight"].shape[2]
+    t.update(page_table=table, pos=None)
+    w = torch.zeros(1, 1, cap, device="cuda")
+    w[:, :, :old] = t["weight"]
+    t["weight"] = w
+    x = H.tokens(torch, rng, [2], 8, 1, 64, "bf16")
+    assert ev.tree_attention_workspace(H.cache_of(ev, t), 8, 2, cap,
+                                       True) < 1 << 30
+    check(t, x, "bf16", decay=0.5)
+
+
 def test_offsets_past_32_bits():
     """Pages more than 2^32 bytes from the pool's start."""
     import torch
