@@ -184,22 +184,25 @@ constexpr int kEvCopies = 4;
 // keys of one digit's bin that are kept as a list, with their slots
 constexpr int kEvList = 4096;
 
-// Sum over the lanes before this one, and over all (wave-uniform).
-__device__ __forceinline__ uint32_t lanes_before(uint32_t x, int lane,
-                                                 uint32_t* all) {
-  uint32_t run = x;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const uint32_t up = __shfl_up(run, o);
-    if (lane >= o) run += up;
-  }
-  *all = __builtin_amdgcn_readlane(run, 63);
-  return run - x;
+// Sum over the lanes before this one, and over all (wave-uniform). Lanes add
+// their neighbours 1, 2, 4 and 8 below within a row of 16, then the last lane of
+// the rows below: six additions in registers, where shuffles through LDS took
+// 0.3 us.
+__device__ __forceinline__ uint32_t lanes_before(uint32_t x, uint32_t* all) {
+  int s = (int)x;
+  s += __builtin_amdgcn_update_dpp(0, s, 0x111, 0xF, 0xF, false);
+  s += __builtin_amdgcn_update_dpp(0, s, 0x112, 0xF, 0xF, false);
+  s += __builtin_amdgcn_update_dpp(0, s, 0x114, 0xF, 0xF, false);
+  s += __builtin_amdgcn_update_dpp(0, s, 0x118, 0xF, 0xF, false);
+  s += __builtin_amdgcn_update_dpp(0, s, 0x142, 0xA, 0xF, false);
+  s += __builtin_amdgcn_update_dpp(0, s, 0x143, 0xC, 0xF, false);
+  *all = (uint32_t)__builtin_amdgcn_readlane(s, 63);
+  return (uint32_t)s - x;
 }
 
 // Keys of a long cache, and the histogram of their first digit, kEvChunk slots
 // a work-group: what one work-group does alone in 16 us for 65,664 slots, with
-// the same again in both passes that follow (44 us in all, 37 so).
+// the same again in both passes that follow (44 us in all, 35 so).
 constexpr int kEvChunk = 4096;
 constexpr int kKeyThreads = 256;
 __global__ __launch_bounds__(kKeyThreads) void evict_keys_kernel(
@@ -261,7 +264,7 @@ __global__ __launch_bounds__(kKeyThreads) void evict_keys_kernel(
 // runs before hold and writes its own into the two lists, 256 slots at a time.
 // LDS: the keys stay there between the passes. Otherwise evict_keys_kernel has
 // left them in the workspace, with the first digit's histograms by chunk.
-// 2,056 slots 10 us, 16,512 16 us, 65,664 33 us and 5 for the keys: a chain of
+// 2,056 slots 8 us, 16,512 13 us, 65,664 30 us and 5 for the keys: a chain of
 // passes and barriers, of which a long cache adds VALU and LDS time.
 template <bool LDS>
 __global__ __launch_bounds__(kEvThreads) void evict_select_kernel(
@@ -321,13 +324,11 @@ __global__ __launch_bounds__(kEvThreads) void evict_select_kernel(
       n[u] = h[0] + h[1] + h[2] + h[3];
     }
     uint32_t all;
-    uint32_t before = lanes_before(n[0] + n[1], lane, &all);
+    uint32_t before = lanes_before(n[0] + n[1], &all);
     if (lane == 0) wave_tot[wave] = all;
     __syncthreads();
-    uint32_t t = lane < wave ? wave_tot[lane] : 0u;   // (16 wavefronts)
-#pragma unroll
-    for (int o = 1; o < 16; o <<= 1) t += __shfl_xor(t, o);
-    before += __builtin_amdgcn_readfirstlane(t);
+    lanes_before(lane < wave ? wave_tot[lane] : 0u, &all);
+    before += all;
     if (before < need && before + n[0] >= need) {
       found[0] = kEvBins - 1 - 2 * tid;
       found[1] = before;
@@ -409,6 +410,7 @@ __global__ __launch_bounds__(kEvThreads) void evict_select_kernel(
       gt &= in;
       lo += __popc(gt & low);
       hi += __popc(gt & ~low);
+      // (one key at a time: the additions of a wavefront become one)
       for (eq &= in; eq; eq &= eq - 1) {
         const int u = __builtin_ctz(eq);
         const uint32_t at = atomicAdd(&listed, 1u);
@@ -418,14 +420,12 @@ __global__ __launch_bounds__(kEvThreads) void evict_select_kernel(
         }
       }
     });
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      lo += __shfl_xor(lo, o);
-      hi += __shfl_xor(hi, o);
-    }
+    uint32_t all_lo, all_hi;
+    lanes_before((uint32_t)lo, &all_lo);
+    lanes_before((uint32_t)hi, &all_hi);
     if (lane == 0) {
-      runs[0][wave] = lo;
-      runs[2][wave] = hi;
+      runs[0][wave] = (int)all_lo;
+      runs[2][wave] = (int)all_hi;
     }
   }
   clear();
@@ -464,21 +464,25 @@ __global__ __launch_bounds__(kEvThreads) void evict_select_kernel(
   });
   __syncthreads();
 
-  // what the runs before this one hold: equal keys, holes, kept tail slots
-  int eqs = 0, holes = 0, tails = 0, all_eq = 0;
-#pragma unroll
-  for (int u = 0; u < kEvWaves; ++u) {
-    const int ua = min(u * per, len), ub = min(ua + per, len);
-    const int below = max(0, min(ub, e.budget) - ua);
-    const int e0 = runs[1][u], e1 = runs[3][u];
-    const int k0 = min(max((int)need - all_eq, 0), e0);
-    const int k1 = min(max((int)need - all_eq - e0, 0), e1);
-    all_eq += e0 + e1;
-    if (u < wave) {
-      eqs = all_eq;
-      holes += below - runs[0][u] - k0;
-      tails += runs[2][u] + k1;
-    }
+  // what the runs before this one hold: equal keys, holes, kept tail slots; a
+  // run a lane
+  int eqs, holes, tails, all_eq;
+  {
+    const bool is = lane < kEvWaves;
+    const int ua = min(lane * per, len), ub = min(ua + per, len);
+    const int below = is ? max(0, min(ub, e.budget) - ua) : 0;
+    const int g0 = is ? runs[0][lane] : 0, e0 = is ? runs[1][lane] : 0;
+    const int g1 = is ? runs[2][lane] : 0, e1 = is ? runs[3][lane] : 0;
+    uint32_t all;
+    const int before = (int)lanes_before((uint32_t)(e0 + e1), &all);
+    all_eq = (int)all;
+    const int k0 = min(max((int)need - before, 0), e0);
+    const int k1 = min(max((int)need - before - e0, 0), e1);
+    const int h = (int)lanes_before((uint32_t)(below - g0 - k0), &all);
+    const int s = (int)lanes_before((uint32_t)(g1 + k1), &all);
+    eqs = __builtin_amdgcn_readlane(before, wave);
+    holes = __builtin_amdgcn_readlane(h, wave);
+    tails = __builtin_amdgcn_readlane(s, wave);
   }
   int32_t* to = e.to + (int64_t)unit * e.max_moves;
   int32_t* from = e.from + (int64_t)unit * e.max_moves;
@@ -497,7 +501,7 @@ __global__ __launch_bounds__(kEvThreads) void evict_select_kernel(
       same &= in;
       uint32_t all;
       int left = (int)need - eqs -
-                 (int)lanes_before((uint32_t)__popc(same), lane, &all);
+                 (int)lanes_before((uint32_t)__popc(same), &all);
       eqs += (int)all;
       for (; same; same &= same - 1)
         if (left-- <= 0) keep &= ~(same & -same);
@@ -505,7 +509,7 @@ __global__ __launch_bounds__(kEvThreads) void evict_select_kernel(
     uint32_t out = in & low & ~keep, tail = keep & ~low;
     uint32_t all;
     const uint32_t at = lanes_before(
-        (uint32_t)__popc(out) | (uint32_t)__popc(tail) << 16, lane, &all);
+        (uint32_t)__popc(out) | (uint32_t)__popc(tail) << 16, &all);
     int h = holes + (int)(at & 0xFFFFu), s = tails + (int)(at >> 16);
     for (; out; out &= out - 1) to[h++] = i + __builtin_ctz(out);
     for (; tail; tail &= tail - 1) from[s++] = i + __builtin_ctz(tail);
