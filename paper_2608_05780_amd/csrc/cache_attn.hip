@@ -9,7 +9,6 @@ namespace evisel {
 namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kMaxTree = 64;
 constexpr int kMaxSplits = 128;   // parts that a row is joined from
